@@ -133,7 +133,7 @@ def _encode(v):
     idx = torch.zeros(a.shape, dtype=torch.uint8, device="cuda")
     for mid in (0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0):
         idx += a > mid
-    idx = (idx + 8 * (b < 0)).view(n, d)
+    idx = (idx + 8 * (b < 0).to(torch.uint8)).view(n, d)
     return idx[:, 0::2] + 16 * idx[:, 1::2], (e + 127.0).to(torch.uint8)
 
 
@@ -240,7 +240,9 @@ def _run_plain(s):
             return out
         amax = y.abs().amax(1, keepdim=True)
         s_x = amax / 127.0
-        q = torch.round(y * (127.0 / amax)).clamp(-127, 127)
+        # a division of tensors: a number over a tensor is formed through
+        # the rounded reciprocal, which moves codes next to a border
+        q = torch.round(y * torch.div(torch.full_like(amax, 127.0), amax)).clamp(-127, 127)
         return out | {"values": (q * s_x).to(torch.bfloat16), "s_x": s_x[:, 0]}
     x = _mx4_decode(s["cx"], s["ex"])
     w = _mx4_decode(s["cw"], s["ew"])
