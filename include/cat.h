@@ -412,6 +412,129 @@ int cat_sqnr_terms(const float* s_x, int64_t n, int bits_x,
                    const void* T, int t_dtype, const double* W_prime,
                    int64_t d_out, int bits_w, double sum_y2, double* out);
 
+/* ------------------------------------------------------------------
+ * RMS norm with the residual's addition in front of a quantized linear (no
+ * passage of the paper: the step of a transformer layer that produces the
+ * layer's input x of Sec. 3, eq. 5).  For every token t:
+ *   h    = fl(x + residual)       (fp32; h = x without a residual)
+ *   residual_out = h rounded to x_dtype (ties to even)
+ *   r    = fl32(1 / sqrt((sum_i h_i^2) / d + eps))     (sum in fp64)
+ *   y_i  = fl(fl(h_i * weight_i) * r)                  (fp32)
+ * y is not stored but quantized: the norm takes the unrounded h.
+ *
+ * cat_rmsnorm_quant: per-token int8 codes with the arithmetic of
+ *   cat_transform_quant at 8 bits (amax = max |y|, s_x = fl(amax / 127),
+ *   code = clamp(rint(fl(y * fl(127 / amax))), -127, 127)): the operand of
+ *   cat_int8_linear.  A token with amax == 0 gets s_x = 0 and zero codes;
+ *   one with a NaN or an infinity in h (or in fl(h * weight)) gets s_x = NaN
+ *   and zero codes, so that its outputs are NaN.
+ * cat_rmsnorm_mx4: MXFP4 codes and scales of y with the arithmetic of
+ *   cat_mx4_quant: the operand of cat_mx4_linear.
+ *
+ * x         device [n x d], x_dtype.  n >= 1; d >= 1, and d % 32 == 0 for
+ *           cat_rmsnorm_mx4.
+ * residual  device [n x d], x_dtype, or NULL (then residual_out is NULL).
+ * residual_out  device [n x d], x_dtype, written; may be `residual` or `x`
+ *           itself (no other overlap).
+ * weight    device [d], w_dtype.
+ * eps       >= 0, finite.  (Where the mean of squares and eps are both 0, y
+ *           = 0.)
+ * codes     device, written: int8 [n x d], or uint8 [n x d/2] (MXFP4).
+ * s_x       device fp32 [n], scales  device uint8 [n x d/32]; written.
+ * Pointers are 16-byte aligned.  No workspace.  The calls may be captured
+ * into a HIP graph.
+ * Errors: CAT_ERR_INVALID_ARG (NULL pointers, dtypes, sizes, eps,
+ * alignment), CAT_ERR_HIP.
+ */
+int cat_rmsnorm_quant(const void* x, int x_dtype, int64_t n, int64_t d,
+                      const void* residual, void* residual_out,
+                      const void* weight, int w_dtype, double eps,
+                      int8_t* codes, float* s_x, void* stream);
+int cat_rmsnorm_mx4(const void* x, int x_dtype, int64_t n, int64_t d,
+                    const void* residual, void* residual_out,
+                    const void* weight, int w_dtype, double eps,
+                    uint8_t* codes, uint8_t* scales, void* stream);
+
+/* ------------------------------------------------------------------
+ * MXFP4: the 4-bit microscaled floating-point format of the OCP
+ * Microscaling Formats (MX) specification v1.0, the floating-point
+ * counterpart of the INT4 codes above.  Every 32 consecutive elements of a
+ * row share a scale 2^e, stored as the byte e + 127 (E8M0; 255 is NaN); an
+ * element is E2M1: sign, two exponent bits and one mantissa bit, values 0,
+ * 0.5, 1, 1.5, 2, 3, 4, 6.  Byte j of a row holds element 2j in bits 0-3 and
+ * element 2j+1 in bits 4-7.
+ *
+ * cat_mx4_quant, for each block of 32:
+ *   amax = max |x_i|
+ *   e    = max(floor(log2 amax) - 2, -127)       (-127 where amax == 0)
+ *   code = x_i / 2^e rounded to E2M1, ties to the even code, magnitudes
+ *          above 6 to 6; the sign of x_i is kept, also for zero
+ *   A block with a NaN or an infinity gets the scale byte 255 and zero
+ *   codes: all its values are NaN.
+ * cat_mx4_dequant: out = value * 2^e, exact in fp32 and bf16 (infinite where
+ *   it exceeds their range), NaN in a block whose scale byte is 255.
+ *
+ * X       device [n x d], x_dtype; out device [n x d], out_dtype, written.
+ * n       >= 1.  d  a positive multiple of 32.
+ * codes   device uint8 [n x d/2], scales device uint8 [n x d/32].
+ * Pointers are 16-byte aligned, buffers do not overlap.  The calls may be
+ * captured into a HIP graph.
+ */
+int cat_mx4_quant(const void* X, int x_dtype, int64_t n, int64_t d,
+                  uint8_t* codes, uint8_t* scales, void* stream);
+int cat_mx4_dequant(const uint8_t* codes, const uint8_t* scales, int64_t n,
+                    int64_t d, void* out, int out_dtype, void* stream);
+
+/* Product of MXFP4 codes (Sec. 3, eq. 5, Q(W T^-1) Q(T x), in that format):
+ *   y[t, o] = sum_j x[t, j] * w[o, j]
+ * of the values the codes stand for; products are exact, sums fp32 (in an
+ * order that depends on the sizes only: repeated calls give identical
+ * bits), y rounded once to y_dtype.
+ * codes_x  device uint8 [n x d_in/2], scales_x device uint8 [n x d_in/32].
+ * codes_w  device uint8 [d_out x d_in/2], scales_w device uint8
+ *          [d_out x d_in/32].
+ * n, d_out in [1, 2^30]; d_in a positive multiple of 32, at most
+ *          CAT_MAX_D_IN.
+ * y        device y_dtype [n x d_out] (written; no overlap with inputs).
+ * A scale byte of 255 makes every output of its row (or column) NaN.
+ * Pointers are 16-byte aligned.  No workspace.  The call may be captured
+ * into a HIP graph.
+ * Errors: CAT_ERR_INVALID_ARG, CAT_ERR_UNSUPPORTED (d_in, n or d_out beyond
+ * the limits), CAT_ERR_HIP.
+ */
+int cat_mx4_linear(const uint8_t* codes_x, const uint8_t* scales_x,
+                   const uint8_t* codes_w, const uint8_t* scales_w, int64_t n,
+                   int64_t d_in, int64_t d_out, void* y, int y_dtype,
+                   void* stream);
+
+/* The same product for rows grouped by expert: row i of the m output rows
+ * belongs to the expert g with offsets[g] <= i < offsets[g + 1] and is
+ *   y[i, o] = sum_j x[src(i), j] * w[g][o, j],
+ * src(i) = row_ids[i], or i when row_ids is NULL.
+ * n        rows of codes_x and scales_x (>= m when row_ids is NULL).
+ * row_ids  device int32 [m] with values in [0, n), in any order and with
+ *          repetitions (a token's row may feed several experts), or NULL.
+ * m        rows of y, >= 1.
+ * offsets  device int32 [groups + 1], non-decreasing, 0 <= offsets[g] <= m.
+ *          Experts may have no rows.  Rows of y before offsets[0] and from
+ *          offsets[groups] on are left as they were.
+ * groups   1 <= groups <= CAT_MAX_GROUPS.
+ * codes_w  device uint8 [groups x d_out x d_in/2], scales_w device uint8
+ *          [groups x d_out x d_in/32].
+ * offsets and row_ids are read on the device, so the call needs no
+ * synchronisation and may be captured and replayed with other values; n, m
+ * and the values are not checked against each other there.  Values outside
+ * the ranges above give undefined rows, but no access outside the buffers.
+ * m <= 2^30.  Other arguments and errors as cat_mx4_linear.
+ */
+#define CAT_MAX_GROUPS 4096
+int cat_mx4_linear_grouped(const uint8_t* codes_x, const uint8_t* scales_x,
+                           int64_t n, const int32_t* row_ids, int64_t m,
+                           const int32_t* offsets, int64_t groups,
+                           const uint8_t* codes_w, const uint8_t* scales_w,
+                           int64_t d_in, int64_t d_out, void* y, int y_dtype,
+                           void* stream);
+
 /* Thread-local message describing the last non-OK return on this thread. */
 const char* cat_last_error(void);
 

@@ -38,6 +38,7 @@ CAT_BUILD_CAT = 3
 
 CAT_MAX_D_IN = 131072
 CAT_MAX_BLOCK = 512
+CAT_MAX_GROUPS = 4096
 
 # every symbol include/cat.h declares
 EXPORTED = (
@@ -48,7 +49,8 @@ EXPORTED = (
     "cat_transform_quant_asym", "cat_w4a4_linear_asym",
     "cat_weight_code_sums", "cat_sqnr_terms", "cat_transform_quant_full_workspace_bytes",
     "cat_transform_quant_full", "cat_full_hadamard_weights", "cat_sqnr_workspace_bytes", "cat_sqnr", "cat_build_transform",
-    "cat_quantize_weights", "cat_last_error", "cat_version",
+    "cat_quantize_weights", "cat_rmsnorm_quant", "cat_rmsnorm_mx4", "cat_mx4_quant",
+    "cat_mx4_dequant", "cat_mx4_linear", "cat_mx4_linear_grouped", "cat_last_error", "cat_version",
 )
 
 
@@ -130,6 +132,18 @@ def lib() -> ctypes.CDLL:
     L.cat_build_transform.restype = _int
     L.cat_quantize_weights.argtypes = [_vp, _i64, _i64, _int, _vp, _vp]
     L.cat_quantize_weights.restype = _int
+    for fn in (L.cat_rmsnorm_quant, L.cat_rmsnorm_mx4):
+        fn.argtypes = [_vp, _int, _i64, _i64, _vp, _vp, _vp, _int, ctypes.c_double, _vp, _vp, _vp]
+        fn.restype = _int
+    L.cat_mx4_quant.argtypes = [_vp, _int, _i64, _i64, _vp, _vp, _vp]
+    L.cat_mx4_quant.restype = _int
+    L.cat_mx4_dequant.argtypes = [_vp, _vp, _i64, _i64, _vp, _int, _vp]
+    L.cat_mx4_dequant.restype = _int
+    L.cat_mx4_linear.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _int, _vp]
+    L.cat_mx4_linear.restype = _int
+    L.cat_mx4_linear_grouped.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64,
+                                         _vp, _int, _vp]
+    L.cat_mx4_linear_grouped.restype = _int
     L.cat_last_error.argtypes = []
     L.cat_last_error.restype = ctypes.c_char_p
     L.cat_version.argtypes = []
@@ -508,6 +522,168 @@ def cat_full_hadamard_weights(W_prime, k: int):
     _check("cat_full_hadamard_weights",
            lib().cat_full_hadamard_weights(pw, d_out, d_in, k, out.ctypes.data))
     return out
+
+
+def _one_device(stream, first, *others):
+    """Every tensor on one device, and that device the current one: kernels
+    are launched there, on the current stream or on `stream`."""
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
+    torch = _torch()
+    current = _current_device() if _current_device is not None else torch.cuda.current_device()
+    if dev.index != current:
+        raise ValueError(f"tensors on {dev}, but the current device is cuda:{current}")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"tensors on {dev}, stream on {stream.device}")
+
+
+def _rmsnorm_args(x, weight, codes, scales, residual, residual_out, stream):
+    """Checks shared by the RMS norm calls; (n, d, pointers of x, residual,
+    residual_out and weight)."""
+    torch = _torch()
+    floats = (torch.bfloat16, torch.float32)
+    px = _dev_ptr(x, "x", floats)
+    pw = _dev_ptr(weight, "weight", floats)
+    if x.dim() != 2:
+        raise ValueError("x must be [n, d]")
+    n, d = x.shape
+    _numel(weight, d, "weight")
+    pr = _dev_ptr(residual, "residual", (x.dtype,), allow_none=True)
+    po = _dev_ptr(residual_out, "residual_out", (x.dtype,), allow_none=True)
+    if (pr is None) != (po is None):
+        raise ValueError("residual and residual_out go together")
+    if pr is not None:
+        _shape(residual, (n, d), "residual")
+        _shape(residual_out, (n, d), "residual_out")
+    _one_device(stream, x, weight, codes, scales, residual, residual_out)
+    return n, d, px, pr, po, pw
+
+
+def cat_rmsnorm_quant(x, weight, codes, s_x, residual=None, residual_out=None, eps: float = 1e-6,
+                      stream=None):
+    """codes int8 [n, d] and s_x [n] fp32 of the RMS norm of h = x +
+    residual times weight [d]; residual_out (which may be residual or x)
+    receives h in x's dtype.  x, residual [n, d] bf16 or fp32."""
+    torch = _torch()
+    pc = _dev_ptr(codes, "codes", (torch.int8,))
+    ps = _dev_ptr(s_x, "s_x", (torch.float32,))
+    n, d, px, pr, po, pw = _rmsnorm_args(x, weight, codes, s_x, residual, residual_out, stream)
+    _shape(codes, (n, d), "codes")
+    _numel(s_x, n, "s_x")
+    _check("cat_rmsnorm_quant",
+           lib().cat_rmsnorm_quant(px, _dtype_code(x), n, d, pr, po, pw, _dtype_code(weight), eps,
+                                   pc, ps, _stream_ptr(stream)))
+
+
+def cat_rmsnorm_mx4(x, weight, codes, scales, residual=None, residual_out=None, eps: float = 1e-6,
+                    stream=None):
+    """cat_rmsnorm_quant with MXFP4 output: codes uint8 [n, d/2] and scales
+    uint8 [n, d/32]."""
+    torch = _torch()
+    pc = _dev_ptr(codes, "codes", (torch.uint8,))
+    ps = _dev_ptr(scales, "scales", (torch.uint8,))
+    n, d, px, pr, po, pw = _rmsnorm_args(x, weight, codes, scales, residual, residual_out, stream)
+    _mx4_shapes(codes, scales, (n,), d)
+    _check("cat_rmsnorm_mx4",
+           lib().cat_rmsnorm_mx4(px, _dtype_code(x), n, d, pr, po, pw, _dtype_code(weight), eps,
+                                 pc, ps, _stream_ptr(stream)))
+
+
+def _mx4_shapes(codes, scales, lead, d, names=("codes", "scales")):
+    if d % 32:
+        raise ValueError(f"rows of {d} elements are not whole blocks of 32")
+    _shape(codes, (*lead, d // 2), names[0])
+    _shape(scales, (*lead, d // 32), names[1])
+
+
+def cat_mx4_quant(X, codes, scales, stream=None):
+    """MXFP4 codes uint8 [n, d/2] and scales uint8 [n, d/32] of X [n, d]
+    (bf16 or fp32; activations or weights)."""
+    torch = _torch()
+    px = _dev_ptr(X, "X", (torch.bfloat16, torch.float32))
+    pc = _dev_ptr(codes, "codes", (torch.uint8,))
+    ps = _dev_ptr(scales, "scales", (torch.uint8,))
+    if X.dim() != 2:
+        raise ValueError("X must be [n, d]")
+    n, d = X.shape
+    _mx4_shapes(codes, scales, (n,), d)
+    _one_device(stream, X, codes, scales)
+    _check("cat_mx4_quant",
+           lib().cat_mx4_quant(px, _dtype_code(X), n, d, pc, ps, _stream_ptr(stream)))
+
+
+def cat_mx4_dequant(codes, scales, out, stream=None):
+    """out [n, d] (bf16 or fp32): the values of MXFP4 codes and scales."""
+    torch = _torch()
+    pc = _dev_ptr(codes, "codes", (torch.uint8,))
+    ps = _dev_ptr(scales, "scales", (torch.uint8,))
+    po = _dev_ptr(out, "out", (torch.bfloat16, torch.float32))
+    if out.dim() != 2:
+        raise ValueError("out must be [n, d]")
+    n, d = out.shape
+    _mx4_shapes(codes, scales, (n,), d)
+    _one_device(stream, codes, scales, out)
+    _check("cat_mx4_dequant",
+           lib().cat_mx4_dequant(pc, ps, n, d, po, _dtype_code(out), _stream_ptr(stream)))
+
+
+def cat_mx4_linear(codes_x, scales_x, codes_w, scales_w, y, stream=None):
+    """y [n, d_out] (bf16 or fp32) = x w^T of MXFP4 codes_x [n, d_in/2] and
+    codes_w [d_out, d_in/2] with their scales [.., d_in/32]."""
+    torch = _torch()
+    u8 = (torch.uint8,)
+    pcx = _dev_ptr(codes_x, "codes_x", u8)
+    psx = _dev_ptr(scales_x, "scales_x", u8)
+    pcw = _dev_ptr(codes_w, "codes_w", u8)
+    psw = _dev_ptr(scales_w, "scales_w", u8)
+    py = _dev_ptr(y, "y", (torch.bfloat16, torch.float32))
+    if codes_x.dim() != 2 or codes_w.dim() != 2:
+        raise ValueError("codes_x and codes_w must be 2-D")
+    n, half = codes_x.shape
+    d_out = codes_w.shape[0]
+    _mx4_shapes(codes_x, scales_x, (n,), 2 * half, ("codes_x", "scales_x"))
+    _mx4_shapes(codes_w, scales_w, (d_out,), 2 * half, ("codes_w", "scales_w"))
+    _shape(y, (n, d_out), "y")
+    _one_device(stream, codes_x, scales_x, codes_w, scales_w, y)
+    _check("cat_mx4_linear",
+           lib().cat_mx4_linear(pcx, psx, pcw, psw, n, 2 * half, d_out, py, _dtype_code(y),
+                                _stream_ptr(stream)))
+
+
+def cat_mx4_linear_grouped(codes_x, scales_x, offsets, codes_w, scales_w, y, row_ids=None,
+                           stream=None):
+    """y [m, d_out] (bf16 or fp32) by experts: rows offsets[g] to offsets[g +
+    1] (int32 [groups + 1]) times the weights codes_w[g] of [groups, d_out,
+    d_in/2].  Row i of y takes row i of codes_x [n, d_in/2], n >= m, or row
+    row_ids[i] (int32 [m])."""
+    torch = _torch()
+    u8 = (torch.uint8,)
+    pcx = _dev_ptr(codes_x, "codes_x", u8)
+    psx = _dev_ptr(scales_x, "scales_x", u8)
+    pof = _dev_ptr(offsets, "offsets", (torch.int32,))
+    pcw = _dev_ptr(codes_w, "codes_w", u8)
+    psw = _dev_ptr(scales_w, "scales_w", u8)
+    pid = _dev_ptr(row_ids, "row_ids", (torch.int32,), allow_none=True)
+    py = _dev_ptr(y, "y", (torch.bfloat16, torch.float32))
+    if codes_x.dim() != 2 or codes_w.dim() != 3 or y.dim() != 2:
+        raise ValueError("codes_x and y must be 2-D, codes_w 3-D")
+    n, half = codes_x.shape
+    groups, d_out, _ = codes_w.shape
+    m = y.shape[0]
+    _mx4_shapes(codes_x, scales_x, (n,), 2 * half, ("codes_x", "scales_x"))
+    _mx4_shapes(codes_w, scales_w, (groups, d_out), 2 * half, ("codes_w", "scales_w"))
+    _shape(y, (m, d_out), "y")
+    _numel(offsets, groups + 1, "offsets")
+    if pid is not None:
+        _numel(row_ids, m, "row_ids")
+    elif n < m:
+        raise ValueError(f"y has {m} rows, codes_x only {n}, and there are no row_ids")
+    _one_device(stream, codes_x, scales_x, offsets, codes_w, scales_w, y, row_ids)
+    _check("cat_mx4_linear_grouped",
+           lib().cat_mx4_linear_grouped(pcx, psx, n, pid, m, pof, groups, pcw, psw, 2 * half, d_out,
+                                        py, _dtype_code(y), _stream_ptr(stream)))
 
 
 def cat_sqnr_workspace_bytes(count: int) -> int:

@@ -3,6 +3,7 @@
 // host before anything is enqueued; nothing falls back silently.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <exception>
 #include <mutex>
 #include <string>
@@ -390,6 +391,172 @@ extern "C" int cat_int8_linear(const int8_t* codes_x, const float* s_x, const in
                                float* y_tilde, int32_t* acc_out, void* stream) {
     return linear_call("cat_int8_linear", true, codes_x, s_x, codes_w, s_w, n, d_in, d_out,
                        y_tilde, acc_out, stream);
+}
+
+// Shared checks of the RMS norm calls; mx4 selects the output format.
+static int rmsnorm_call(const char* fn, const void* x, int x_dtype, int64_t n, int64_t d,
+                        const void* residual, void* residual_out, const void* weight, int w_dtype,
+                        double eps, int mx4, uint8_t* codes, void* scales, void* stream) {
+    try {
+        if (!x || !weight || !codes || !scales)
+            return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": NULL pointer");
+        if (!residual != !residual_out)
+            return fail(CAT_ERR_INVALID_ARG,
+                        std::string(fn) + ": residual and residual_out go together");
+        if (!valid_dtype(x_dtype) || !valid_dtype(w_dtype))
+            return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": bad dtype");
+        if (n < 1 || d < 1) return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": n and d must be >= 1");
+        if (mx4 && d % 32) return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": d % 32 != 0");
+        if (!(eps >= 0.0) || !std::isfinite(eps))
+            return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": eps must be finite and >= 0");
+        if (!cat::aligned16(x) || !cat::aligned16(residual) || !cat::aligned16(residual_out) ||
+            !cat::aligned16(weight) || !cat::aligned16(codes) || !cat::aligned16(scales))
+            return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": pointers must be 16-byte aligned");
+        if (int rc = require_device(fn)) return rc;
+        const hipError_t err =
+            catk::launch_rmsnorm(x, x_dtype == CAT_BF16, n, d, residual, residual_out, weight,
+                                 w_dtype == CAT_BF16, eps, mx4, codes, scales,
+                                 static_cast<hipStream_t>(stream));
+        if (err != hipSuccess) return hip_fail(fn, err);
+        return CAT_OK;
+    } catch (const std::exception& e) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": " + e.what());
+    } catch (...) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": unknown error");
+    }
+}
+
+extern "C" int cat_rmsnorm_quant(const void* x, int x_dtype, int64_t n, int64_t d,
+                                 const void* residual, void* residual_out, const void* weight,
+                                 int w_dtype, double eps, int8_t* codes, float* s_x, void* stream) {
+    return rmsnorm_call("cat_rmsnorm_quant", x, x_dtype, n, d, residual, residual_out, weight,
+                        w_dtype, eps, 0, reinterpret_cast<uint8_t*>(codes), s_x, stream);
+}
+
+extern "C" int cat_rmsnorm_mx4(const void* x, int x_dtype, int64_t n, int64_t d,
+                               const void* residual, void* residual_out, const void* weight,
+                               int w_dtype, double eps, uint8_t* codes, uint8_t* scales,
+                               void* stream) {
+    return rmsnorm_call("cat_rmsnorm_mx4", x, x_dtype, n, d, residual, residual_out, weight,
+                        w_dtype, eps, 1, codes, scales, stream);
+}
+
+// Shared checks of the MXFP4 conversions.
+static int mx4_convert_check(const char* fn, const void* values, int dtype, int64_t n, int64_t d,
+                             const void* codes, const void* scales) {
+    if (!values || !codes || !scales)
+        return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": NULL pointer");
+    if (!valid_dtype(dtype)) return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": bad dtype");
+    if (n < 1 || d < 1) return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": n and d must be >= 1");
+    if (d % 32) return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": d % 32 != 0");
+    if (!cat::aligned16(values) || !cat::aligned16(codes) || !cat::aligned16(scales))
+        return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": pointers must be 16-byte aligned");
+    return require_device(fn);
+}
+
+extern "C" int cat_mx4_quant(const void* X, int x_dtype, int64_t n, int64_t d, uint8_t* codes,
+                             uint8_t* scales, void* stream) {
+    const char* fn = "cat_mx4_quant";
+    try {
+        if (int rc = mx4_convert_check(fn, X, x_dtype, n, d, codes, scales)) return rc;
+        const hipError_t err = catk::launch_mx4_quant(X, x_dtype == CAT_BF16, n, d, codes, scales,
+                                                      static_cast<hipStream_t>(stream));
+        if (err != hipSuccess) return hip_fail(fn, err);
+        return CAT_OK;
+    } catch (const std::exception& e) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": " + e.what());
+    } catch (...) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": unknown error");
+    }
+}
+
+extern "C" int cat_mx4_dequant(const uint8_t* codes, const uint8_t* scales, int64_t n, int64_t d,
+                               void* out, int out_dtype, void* stream) {
+    const char* fn = "cat_mx4_dequant";
+    try {
+        if (int rc = mx4_convert_check(fn, out, out_dtype, n, d, codes, scales)) return rc;
+        const hipError_t err = catk::launch_mx4_dequant(codes, scales, n, d, out,
+                                                        out_dtype == CAT_BF16,
+                                                        static_cast<hipStream_t>(stream));
+        if (err != hipSuccess) return hip_fail(fn, err);
+        return CAT_OK;
+    } catch (const std::exception& e) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": " + e.what());
+    } catch (...) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": unknown error");
+    }
+}
+
+// Shared checks of the MXFP4 products; `rows` are the rows of y.
+static int mx4_linear_check(const char* fn, const void* codes_x, const void* scales_x,
+                            const void* codes_w, const void* scales_w, int64_t n, int64_t rows,
+                            int64_t d_in, int64_t d_out, const void* y, int y_dtype) {
+    constexpr int64_t kMost = int64_t{1} << 30;
+    if (!codes_x || !scales_x || !codes_w || !scales_w || !y)
+        return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": NULL pointer");
+    if (n < 1 || rows < 1 || d_in < 1 || d_out < 1)
+        return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": sizes must be >= 1");
+    if (d_in % 32) return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": d_in % 32 != 0");
+    if (!valid_dtype(y_dtype)) return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": bad y_dtype");
+    if (d_in > CAT_MAX_D_IN)
+        return fail(CAT_ERR_UNSUPPORTED, std::string(fn) + ": d_in > CAT_MAX_D_IN");
+    if (n > kMost || rows > kMost || d_out > kMost)
+        return fail(CAT_ERR_UNSUPPORTED, std::string(fn) + ": sizes beyond 2^30");
+    if (!cat::aligned16(codes_x) || !cat::aligned16(scales_x) || !cat::aligned16(codes_w) ||
+        !cat::aligned16(scales_w) || !cat::aligned16(y))
+        return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": pointers must be 16-byte aligned");
+    return CAT_OK;
+}
+
+extern "C" int cat_mx4_linear(const uint8_t* codes_x, const uint8_t* scales_x,
+                              const uint8_t* codes_w, const uint8_t* scales_w, int64_t n,
+                              int64_t d_in, int64_t d_out, void* y, int y_dtype, void* stream) {
+    const char* fn = "cat_mx4_linear";
+    try {
+        if (int rc = mx4_linear_check(fn, codes_x, scales_x, codes_w, scales_w, n, n, d_in, d_out, y,
+                                      y_dtype))
+            return rc;
+        if (int rc = require_device(fn)) return rc;
+        const hipError_t err =
+            catk::launch_mx4_linear(codes_x, scales_x, codes_w, scales_w, n, d_in, d_out, y,
+                                    y_dtype == CAT_BF16, static_cast<hipStream_t>(stream));
+        if (err != hipSuccess) return hip_fail(fn, err);
+        return CAT_OK;
+    } catch (const std::exception& e) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": " + e.what());
+    } catch (...) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": unknown error");
+    }
+}
+
+extern "C" int cat_mx4_linear_grouped(const uint8_t* codes_x, const uint8_t* scales_x, int64_t n,
+                                      const int32_t* row_ids, int64_t m, const int32_t* offsets,
+                                      int64_t groups, const uint8_t* codes_w,
+                                      const uint8_t* scales_w, int64_t d_in, int64_t d_out, void* y,
+                                      int y_dtype, void* stream) {
+    const char* fn = "cat_mx4_linear_grouped";
+    try {
+        if (int rc = mx4_linear_check(fn, codes_x, scales_x, codes_w, scales_w, n, m, d_in, d_out, y,
+                                      y_dtype))
+            return rc;
+        if (!offsets) return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": NULL pointer");
+        if (groups < 1 || groups > CAT_MAX_GROUPS)
+            return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": groups must be in [1, CAT_MAX_GROUPS]");
+        if (!row_ids && n < m)
+            return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": n < m without row_ids");
+        if (!cat::aligned16(offsets) || !cat::aligned16(row_ids))
+            return fail(CAT_ERR_INVALID_ARG, std::string(fn) + ": pointers must be 16-byte aligned");
+        if (int rc = require_device(fn)) return rc;
+        const hipError_t err = catk::launch_mx4_linear_grouped(
+            codes_x, scales_x, n, row_ids, m, offsets, groups, codes_w, scales_w, d_in, d_out, y,
+            y_dtype == CAT_BF16, static_cast<hipStream_t>(stream));
+        if (err != hipSuccess) return hip_fail(fn, err);
+        return CAT_OK;
+    } catch (const std::exception& e) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": " + e.what());
+    } catch (...) {
+        return fail(CAT_ERR_INTERNAL, std::string(fn) + ": unknown error");
+    }
 }
 
 extern "C" size_t cat_sqnr_workspace_bytes(int64_t count) {

@@ -75,6 +75,31 @@ hipError_t launch_split_gemm(int tile, bool i8, const uint8_t* codes_x, const fl
                              int64_t d_out, float* y, int32_t* acc_out, const float* zmin_x,
                              const int32_t* rsum_w, hipStream_t stream);
 
+// ---- MXFP4: codes [n x d/2], scale bytes [n x d/32]; d % 32 == 0
+hipError_t launch_mx4_quant(const void* x, int x_bf16, int64_t n, int64_t d, uint8_t* codes,
+                            uint8_t* scales, hipStream_t stream);
+hipError_t launch_mx4_dequant(const uint8_t* codes, const uint8_t* scales, int64_t n, int64_t d,
+                              void* out, int out_bf16, hipStream_t stream);
+// y [n x d_out] (bf16 or fp32) from codes_x [n x d_in/2], codes_w
+// [d_out x d_in/2] and their scales.
+hipError_t launch_mx4_linear(const uint8_t* cx, const uint8_t* ex, const uint8_t* cw,
+                             const uint8_t* ew, int64_t n, int64_t d_in, int64_t d_out, void* y,
+                             int y_bf16, hipStream_t stream);
+// The same with the m rows of y split over `groups` weight matrices by
+// device offsets [groups + 1]; row i reads codes_x row row_ids[i] (i when
+// row_ids is NULL).
+hipError_t launch_mx4_linear_grouped(const uint8_t* cx, const uint8_t* ex, int64_t n,
+                                     const int32_t* row_ids, int64_t m, const int32_t* offsets,
+                                     int64_t groups, const uint8_t* cw, const uint8_t* ew,
+                                     int64_t d_in, int64_t d_out, void* y, int y_bf16,
+                                     hipStream_t stream);
+
+// ---- RMS norm + residual + quantized output: int8 codes with fp32 scales
+// [n] (mx4 == 0) or MXFP4 codes with scale bytes [n x d/32].
+hipError_t launch_rmsnorm(const void* x, int x_bf16, int64_t n, int64_t d, const void* res,
+                          void* res_out, const void* w, int w_bf16, double eps, int mx4,
+                          uint8_t* codes, void* scales, hipStream_t stream);
+
 // ---- second moment accumulation
 // Workspace of launch_cov_accumulate on the current device (0 when the
 // configuration runs on kernels that need none).
