@@ -187,6 +187,12 @@ def test_linear_tiles(n, d_in, d_out, dtype):
     _linear(n, d_in, d_out, dtype, seed=5)
 
 
+def test_linear_more_tiles_than_workgroups():
+    # each workgroup then walks several tiles, the last round not full
+    _linear(2500, 512, 9000, "bf16", seed=6)
+    _linear(4096, 1024, 4500, "f32", seed=7)
+
+
 @pytest.mark.parametrize("n,d_in,d_out", [(4, 512, 64), (300, 512, 512)])
 def test_linear_wide_scale_range(n, d_in, d_out):
     # scales over 2^+-60: a block then dominates its row
