@@ -3,12 +3,16 @@
 // on the block-scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4:
 // lane L holds row L % 16, elements [32 (L / 16), 32 (L / 16) + 32) of a
 // step of 128 (16 bytes of codes) and that block's scale byte.
+#include <type_traits>
+
 #include "kernels.h"
 #include "mx4_common.h"
 
 namespace catk {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kMxXcd = 8;
 
 // acc += A B for one step; a and b are a lane's 16 bytes of codes, sa and sb
 // their scale bytes (bits 0-7).
@@ -79,9 +83,42 @@ __device__ __forceinline__ bool mx4_rows(const Mx4Args& a, int tile, Mx4Rows& r)
     return false;
 }
 
+// Most row tiles of bm rows that a call can have: every expert with rows may
+// end inside one.
+__host__ __device__ inline int64_t mx4_row_tiles_most(const Mx4Args& a, int bm) {
+    return (a.m + bm - 1) / bm + (a.offsets ? (a.groups < a.m ? a.groups : a.m) : 0);
+}
+
 __device__ __forceinline__ int mx4_source_row(const Mx4Args& a, int i) {
     int s = a.row_ids ? a.row_ids[i] : i;
     return s < 0 ? 0 : (s < a.n ? s : a.n - 1);
+}
+
+// global -> LDS copies as dma16 and dma4 of the common header (16 or 4 bytes a
+// lane, the lane's bytes at lds + 16 or 4 lane), with M0 given up instead of
+// saved: nothing else here keeps a value in it, and a copy is then three
+// instructions.  The first takes a wave-uniform base and a 32-bit offset a
+// lane, the others an address a lane.
+__device__ __forceinline__ void mx4_copy16(const uint8_t* base, uint32_t off, uint32_t lds) {
+    asm volatile(
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds)
+        : "memory", "m0");
+}
+__device__ __forceinline__ void mx4_copy16(const uint8_t* p, uint32_t lds) {
+    asm volatile(
+        "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %0, off" ::"v"(p), "s"(lds)
+        : "memory", "m0");
+}
+__device__ __forceinline__ void mx4_copy4(const uint8_t* p, uint32_t lds) {
+    asm volatile(
+        "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dword %0, off" ::"v"(p), "s"(lds)
+        : "memory", "m0");
 }
 
 __device__ __forceinline__ void mx4_store(float* y, float v) { *y = v; }
@@ -89,43 +126,233 @@ __device__ __forceinline__ void mx4_store(uint16_t* y, float v) {
     *y = static_cast<uint16_t>(pack_bf16(v, 0.0f));
 }
 
-// One wave per 16 outputs x 16 rows, operands straight from global memory.
-template <typename Y>
-__global__ __launch_bounds__(kWave) void mx4_gemm_kernel(Mx4Args a) {
-    Mx4Rows r;
-    if (!mx4_rows<16>(a, static_cast<int>(blockIdx.x), r)) return;
-    const int lane = threadIdx.x, l16 = lane & 15, q = lane >> 4;
-    const int blocks = a.d_in / kMxBlock;
-    const int o = static_cast<int>(blockIdx.y) * 16 + l16;
-    const int oc = o < a.d_out ? o : a.d_out - 1;
-    const int64_t wrow = static_cast<int64_t>(r.group) * a.d_out + oc;
-    const int i = r.first + l16 < r.end ? r.first + l16 : r.end - 1;
-    const int64_t xrow = mx4_source_row(a, i);
-    const u32x4* pw = reinterpret_cast<const u32x4*>(a.cw) + wrow * blocks;
-    const u32x4* px = reinterpret_cast<const u32x4*>(a.cx) + xrow * blocks;
-    const uint8_t* sw = a.ew + wrow * blocks;
-    const uint8_t* sx = a.ex + xrow * blocks;
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int b0 = 0; b0 < blocks; b0 += 4) {
-        const int b = b0 + q;
-        u32x4 cw = {0, 0, 0, 0}, cx = {0, 0, 0, 0};
-        int ew = kMxByteOne, ex = kMxByteOne;
-        if (b < blocks) {
-            cw = pw[b];
-            cx = px[b];
-            ew = sw[b];
-            ex = sx[b];
-        }
-        acc = mx4_mfma(cw, cx, acc, ew, ex);
-    }
-    // lane: row l16 of the tile, outputs 4 q .. 4 q + 3
-    const int row = r.first + l16;
-    if (row >= r.end) return;
-    Y* y = static_cast<Y*>(a.y) + static_cast<int64_t>(row) * a.d_out;
+// -------------------------------------------------- tiles for fewer rows
+// A workgroup of 8 waves owns 16 A rows x 16 B outputs and its waves share
+// out the reduction: wave w takes its w-th eighth of the chunks of 128
+// elements, streams them through an LDS ring of its own (D chunks of A + B
+// KiB of codes and their scale bytes, global -> LDS copies, no barriers), and
+// the 8 partial sums are added in LDS in the waves' order.  A tile's weights
+// are then read by 8 waves at once, so a few rows still keep HBM busy.
+//
+// A chunk's copies: 16 rows x 64 bytes of codes per fragment (four lanes on
+// 64 contiguous bytes; unit u of row r at slot 4 r + (u ^ ((r >> 2) & 3))),
+// and one dword of scale bytes per row, 64 rows a copy.  Rows whose scale
+// bytes are not dword-aligned (d_in % 128 != 0; ALN = false) copy the two
+// aligned dwords that hold them (bytes of the buffers' last dword past its
+// end are read with it, never used) and a lane picks its byte, at a place
+// that depends on its row only.  Units past a row's end count as zero with
+// scale 1.
+constexpr int kSpWaves = 8;
+constexpr int kSpThreads = kSpWaves * kWave;
+
+// LDS of a wave: its ring, later its partial sums of a round of at most 8
+// accumulators.
+constexpr int sp_stage_bytes(int a, int b, bool aligned) {
+    return (a + b) * 1024 + (a + b + 3) / 4 * 256 * (aligned ? 1 : 2);
+}
+constexpr int sp_round(int a, int b) { return a * b < 8 ? a * b : 8; }
+// The ring's depth: D where it fits the LDS, else one less.
+constexpr int sp_depth(int a, int b, int d, bool aligned) {
+    return d * sp_stage_bytes(a, b, aligned) * kSpWaves <= 160 * 1024 ? d : d - 1;
+}
+constexpr int sp_wave_bytes(int a, int b, int d, bool aligned) {
+    return d * sp_stage_bytes(a, b, aligned) > sp_round(a, b) * 1024 ? d * sp_stage_bytes(a, b, aligned)
+                                                                     : sp_round(a, b) * 1024;
+}
+
+template <typename Y, int A, int B, int D, bool ALN>
+__device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& r, int n0,
+                                               uint8_t (&lds)[kSpWaves][sp_wave_bytes(A, B, D, ALN)]) {
+    constexpr int BM = 16 * A, BN = 16 * B;
+    constexpr int L = A + B;               // code copies per chunk
+    constexpr int SC = (L + 3) / 4;        // scale copies per chunk and dword
+    constexpr int COPIES = L + SC * (ALN ? 1 : 2);
+    static_assert(COPIES * (D - 1) < 64, "copies in flight must fit the vmcnt range");
+    constexpr int kScaleAt = L * 1024;     // bytes in a ring stage
+    constexpr int kStageBytes = sp_stage_bytes(A, B, ALN);
+    constexpr int RT = sp_round(A, B);     // accumulators added per round
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int l16 = lane & 15, q = lane >> 4;
+    const uint32_t rb = static_cast<uint32_t>(a.d_in) / 2;
+    const uint32_t sb = static_cast<uint32_t>(a.d_in) / 32;
+    const int nk = (a.d_in + 127) / 128;
+    const int rows_x = r.end - r.first < BM ? r.end - r.first : BM;
+    const int rows_w = a.d_out - n0 < BN ? a.d_out - n0 : BN;
+    const int64_t w0 = static_cast<int64_t>(r.group) * a.d_out + n0;
+    // row i of the tile's tokens (i < BM) or weights (BM + o); rows past the
+    // end read the last one (their results are not stored)
+    auto x_row = [&](int i) {
+        return static_cast<int64_t>(mx4_source_row(a, r.first + (i < rows_x ? i : rows_x - 1)));
+    };
+    auto w_row = [&](int o) { return w0 + (o < rows_w ? o : rows_w - 1); };
+
+    const uint8_t* src[L];
+    const int cr = lane >> 2;
+    const uint32_t cu = 16u * static_cast<uint32_t>((lane & 3) ^ ((lane >> 4) & 3));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int col = static_cast<int>(blockIdx.y) * 16 + 4 * q + e;
-        if (col < a.d_out) mx4_store(y + col, acc[e]);
+    for (int g = 0; g < L; ++g)
+        src[g] = g < A ? a.cx + x_row(16 * g + cr) * rb : a.cw + w_row(16 * (g - A) + cr) * rb;
+    const uint8_t* ssrc[SC];               // scale row of lane's row 64 g + lane
+    const uint8_t* send[SC];               // last aligned dword of its buffer
+#pragma unroll
+    for (int g = 0; g < SC; ++g) {
+        const int i = 64 * g + lane < 16 * L ? 64 * g + lane : 16 * L - 1;
+        const bool x = i < BM;
+        ssrc[g] = x ? a.ex + x_row(i) * sb : a.ew + w_row(i - BM) * sb;
+        if constexpr (!ALN) {
+            const int64_t bytes = x ? static_cast<int64_t>(a.n) * sb
+                                    : static_cast<int64_t>(a.groups) * a.d_out * sb;
+            send[g] = (x ? a.ex : a.ew) + ((bytes - 1) & ~int64_t{3});
+        }
+    }
+    const uint32_t ring = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds_addr(&lds[wave][0])));
+    auto issue = [&](int chunk, int st) {
+        const uint32_t at = ring + static_cast<uint32_t>(st * kStageBytes);
+        uint32_t col = static_cast<uint32_t>(chunk) * 64u + cu;
+        if (!ALN) col = col < rb ? col : 0;        // past the row's end: any unit of it
+#pragma unroll
+        for (int g = 0; g < L; ++g) mx4_copy16(src[g] + col, at + g * 1024u);
+#pragma unroll
+        for (int g = 0; g < SC; ++g) {
+            const uint8_t* p = ssrc[g] + 4 * chunk;
+            if constexpr (ALN) {
+                mx4_copy4(p, at + kScaleAt + g * 256u);
+            } else {
+                const uint64_t lo = reinterpret_cast<uint64_t>(p) & ~uint64_t{3};
+                const uint64_t end = reinterpret_cast<uint64_t>(send[g]);
+                mx4_copy4(reinterpret_cast<const uint8_t*>(lo < end ? lo : end), at + kScaleAt + g * 256u);
+                mx4_copy4(reinterpret_cast<const uint8_t*>(lo + 4 < end ? lo + 4 : end),
+                          at + kScaleAt + (SC + g) * 256u);
+            }
+        }
+    };
+
+    // byte of the lane's scale inside a stage, by fragment
+    int sat[L];
+#pragma unroll
+    for (int g = 0; g < L; ++g) {
+        const int i = 16 * g + l16;
+        int byte = q, dword = 0;
+        if constexpr (!ALN) {
+            const uint64_t row = g < A ? reinterpret_cast<uint64_t>(a.ex) + x_row(i) * sb
+                                       : reinterpret_cast<uint64_t>(a.ew) + w_row(i - BM) * sb;
+            const int at = static_cast<int>(row & 3) + q;
+            byte = at & 3;
+            dword = at >> 2;
+        }
+        sat[g] = kScaleAt + dword * (SC * 256) + 4 * i + byte;
+    }
+    const int slot = 16 * (4 * l16 + (q ^ (l16 >> 2)));
+    u32x4 f[L];
+    int s[L];
+    auto read = [&](int st) {
+        const uint8_t* at = &lds[wave][st * kStageBytes];
+#pragma unroll
+        for (int g = 0; g < L; ++g) {
+            f[g] = *reinterpret_cast<const u32x4*>(at + g * 1024 + slot);
+            s[g] = at[sat[g]];
+        }
+    };
+    f32x4 acc[A][B];
+#pragma unroll
+    for (int i = 0; i < A; ++i)
+#pragma unroll
+        for (int j = 0; j < B; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto compute = [&](int chunk) {
+        if (!ALN && 4 * chunk + q >= static_cast<int>(sb)) {
+#pragma unroll
+            for (int g = 0; g < L; ++g) {
+                s[g] = kMxByteOne;
+                f[g] = u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < A; ++i)
+#pragma unroll
+            for (int j = 0; j < B; ++j) acc[i][j] = mx4_mfma(f[A + j], f[i], acc[i][j], s[A + j], s[i]);
+    };
+    const int cnt = nk > wave ? (nk - wave + kSpWaves - 1) / kSpWaves : 0;
+#pragma unroll
+    for (int st = 0; st < D; ++st)
+        if (st < cnt) issue(wave + st * kSpWaves, st);
+    int i = 0, st = 0;
+    for (; i + D < cnt; ++i) {
+        wait_vmcnt<(D - 1) * COPIES>();
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("" ::: "memory");
+        read(st);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        issue(wave + (i + D) * kSpWaves, st);
+        compute(wave + i * kSpWaves);
+        st = st + 1 == D ? 0 : st + 1;
+    }
+    wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+    for (; i < cnt; ++i) {
+        read(st);
+        compute(wave + i * kSpWaves);
+        st = st + 1 == D ? 0 : st + 1;
+    }
+
+    // partial sums, RT accumulators a round: lane holds row l16, outputs 4 q .. + 3
+    constexpr int ROUNDS = (A * B + RT - 1) / RT;
+#pragma unroll
+    for (int rd = 0; rd < ROUNDS; ++rd) {
+        __syncthreads();                   // the ring (or the last round) is read
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int tl = rd * RT + t;
+            if (tl < A * B)
+                reinterpret_cast<f32x4*>(&lds[wave][0])[t * kWave + lane] = acc[tl / B][tl % B];
+        }
+        __syncthreads();
+        const int tl = rd * RT + wave;
+        if (wave < RT && tl < A * B) {
+            f32x4 v = reinterpret_cast<const f32x4*>(&lds[0][0])[wave * kWave + lane];
+#pragma unroll
+            for (int w = 1; w < kSpWaves; ++w) {
+                const f32x4 p = reinterpret_cast<const f32x4*>(&lds[w][0])[wave * kWave + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += p[e];
+            }
+            const int row = (tl / B) * 16 + l16, col = (tl % B) * 16 + 4 * q;
+            if (row < rows_x && col < rows_w) {
+                Y* y = static_cast<Y*>(a.y) + static_cast<int64_t>(r.first + row) * a.d_out + n0 + col;
+                if ((a.d_out & 3) == 0) {
+                    if constexpr (sizeof(Y) == 4) *reinterpret_cast<f32x4*>(y) = v;
+                    else *reinterpret_cast<u32x2*>(y) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < rows_w) mx4_store(y + e, v[e]);
+                }
+            }
+        }
+    }
+}
+
+template <typename Y, int A, int B, int D, bool ALN>
+__global__ __launch_bounds__(kSpThreads) void mx4_split_kernel(Mx4Args a) {
+    constexpr int BM = 16 * A, BN = 16 * B;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kSpWaves][sp_wave_bytes(A, B, D, ALN)];
+    // XCD x walks one contiguous range of tiles, the row tiles of a column
+    // panel next to each other: its weights then enter that XCD's L2 once
+    const int tiles_n = (a.d_out + BN - 1) / BN;
+    const int64_t row_tiles = mx4_row_tiles_most(a, BM);
+    const int64_t T = row_tiles * tiles_n;
+    const int64_t per_xcd = (T + kMxXcd - 1) / kMxXcd;
+    for (int64_t j = blockIdx.x / kMxXcd; j < per_xcd; j += gridDim.x / kMxXcd) {
+        const int64_t tau = (blockIdx.x % kMxXcd) * per_xcd + j;
+        if (tau >= T) return;
+        const int tn = static_cast<int>(tau / row_tiles);
+        Mx4Rows r;
+        if (!mx4_rows<BM>(a, static_cast<int>(tau - tn * row_tiles), r)) continue;
+        r.group = __builtin_amdgcn_readfirstlane(r.group);
+        r.first = __builtin_amdgcn_readfirstlane(r.first);
+        r.end = __builtin_amdgcn_readfirstlane(r.end);
+        mx4_split_tile<Y, A, B, D, ALN>(a, r, tn * BN, lds);
+        __syncthreads();                   // the sums are read before the next ring
     }
 }
 
@@ -135,33 +362,31 @@ __global__ __launch_bounds__(kWave) void mx4_gemm_kernel(Mx4Args a) {
 // with BM = 256, the accumulation half of the register file), so a fragment
 // read from LDS serves 8 matrix instructions.
 //
-// A stage is 128 elements of the reduction, 64 bytes of every row: one matrix
-// step.  Stages go from global memory into a ring of four LDS buffers with
-// global_load_lds_dwordx4, requested three ahead.  During stage h a wave
-// multiplies its weight fragments (read during h - 1) with the token
-// fragments of h (read three fragments ahead of their use), reads the weight
-// fragments of h + 1 and requests stage h + 3 into the buffer of h - 1.  One
-// barrier a stage: behind it all waves are done with h - 1, and (vmcnt) h + 1
-// has arrived.
+// The reduction goes in pairs of stages. A stage is 128 elements, one matrix
+// step; a pair is 128 bytes of every row, a whole cache line: global -> LDS
+// copies (global_load_lds_dwordx4) of rows of 64 bytes reach 27 to 34 bytes
+// per clock and CU with all CUs reading, of 128 bytes 53.  Two pairs fit the
+// LDS.  In a stage a wave multiplies its 8 weight fragments, read during the
+// stage before, with token fragments that it reads three ahead of their use.
+// After the last token fragment of a pair's second stage has been read there
+// is a barrier: behind it the pair's buffer is free, the next pair but one is
+// requested into it, and (vmcnt) the next pair has arrived.
 //
-// Scale bytes come in 16 a row, four stages, likewise straight into LDS; a
-// lane reads a row's 16 bytes and keeps the four of its block column q (byte
-// 4 s + q for stage s) in one register, whose byte s the matrix instruction
-// of stage s selects.
+// Scale bytes come in 16 a row, two pairs, likewise straight into LDS; a lane
+// keeps the four of its block column in one register, whose byte s the matrix
+// instruction of stage s selects.
 //
-// Workgroups are persistent and their tiles form one stream of stages, so
-// the requests run ahead across tiles; past the last stage they repeat the
-// last tile's first ones, which keeps the stages free of branches.
+// Workgroups are persistent and their tiles form one stream of pairs, so the
+// requests run ahead across tiles; past the last one they repeat the last
+// tile's first ones, which keeps the stages free of branches.
 //
-// LDS: unit u (16 bytes) of row r sits at slot 4 r + (u ^ ((r >> 2) & 3)): a
+// LDS: unit u (16 bytes) of row r sits at slot 8 r + (u ^ ((r >> 1) & 7)): a
 // fragment's 16 rows at one unit fall on 16 different 16-byte bank groups.
 constexpr int kTlThreads = 256;
 constexpr int kTlN = 256;                  // outputs per tile
-constexpr int kTlUnits = 4;                // 16-byte units of a row per stage
-constexpr int kTlStage = 128;              // elements of the reduction per stage
-constexpr int kTlRing = 4;
+constexpr int kTlUnits = 8;                // 16-byte units of a row per pair of stages
+constexpr int kTlPair = 256;               // elements of the reduction per pair
 constexpr int kTlGroupM = 4;               // row panels that are walked together
-constexpr int kMxXcd = 8;
 
 // Row tiles of the call.
 template <int BM>
@@ -204,11 +429,12 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     constexpr int IO = 8;                  // 16-output fragments of a wave
     constexpr int IT = BM / 32;            // 16-row fragments of a wave
     constexpr int ROWS = kTlN + BM;        // LDS rows: weights, then tokens
-    constexpr int LW = kTlN / 64, LX = BM / 64;     // direct loads a wave and stage
+    constexpr int LW = kTlN / 32, LX = BM / 32;     // copies a wave and pair
     constexpr int NL = LW + LX, NM = IO * IT;
     constexpr int XB = 4;                  // token fragments in registers
-    __shared__ __attribute__((aligned(16))) u32x4 codes[kTlRing][ROWS * kTlUnits];
+    __shared__ __attribute__((aligned(16))) u32x4 codes[2][ROWS * kTlUnits];
     __shared__ __attribute__((aligned(16))) u32x4 scales[2][ROWS];
+    __shared__ __attribute__((aligned(16))) u32x4 outs[kTlThreads / kWave][256];
 
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -216,7 +442,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     const int l16 = lane & 15, q = lane >> 4;
     const uint32_t rb = static_cast<uint32_t>(a.d_in) / 2;       // bytes of a code row
     const uint32_t sb = static_cast<uint32_t>(a.d_in) / 32;      // bytes of a scale row
-    const int nk = a.d_in / kTlStage;      // a multiple of 4
+    const int np = a.d_in / kTlPair;       // even
 
     // Tiles are numbered so that each XCD (workgroups are dealt to the 8 of
     // them in turn) walks one contiguous range, kTlGroupM row panels at a
@@ -246,15 +472,15 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         return true;
     };
 
-    // ---- the load cursor: the tile and stage requested next
+    // ---- the load cursor: the tile and pair requested next
     Tile lt{};
     int64_t lk = 0;                        // its number in this workgroup's list
-    int ls = 0;                            // its next stage
+    int ls = 0;                            // its next pair
     if (!tile_at(0, lt)) return;
     Tile tile = lt;
-    // Direct load j of this wave fills the 64 slots of 16 rows: weights' rows
-    // 16 (4 j + wave) .. + 15, then the tokens' likewise.
-    const uint32_t unit = 16u * static_cast<uint32_t>((lane & 3) ^ ((lane >> 4) & 3));
+    // Copy j of this wave fills the 64 slots of 8 rows: weights' rows
+    // 8 (4 j + wave) .. + 7, then the tokens' likewise.
+    const uint32_t unit = 16u * static_cast<uint32_t>((lane & 7) ^ ((lane >> 4) | ((wave & 1) << 2)));
     const uint8_t *base_w, *base_x, *base_sw, *base_sx;
     uint32_t off_w[LW], off_x[LX], off_sw, off_sx;
     auto set_rows = [&]() {
@@ -266,7 +492,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         // rows past the end read the last one (their results are not stored)
 #pragma unroll
         for (int j = 0; j < LW; ++j) {
-            const int r = 16 * (4 * j + wave) + (lane >> 2);
+            const int r = 8 * (4 * j + wave) + (lane >> 3);
             off_w[j] = static_cast<uint32_t>(r < left_w ? r : left_w - 1) * rb + unit;
         }
         const int rw = 64 * wave + lane;
@@ -279,7 +505,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
             return static_cast<uint32_t>(by_id ? mx4_source_row(a, lt.first + c) : c);
         };
 #pragma unroll
-        for (int j = 0; j < LX; ++j) off_x[j] = src(16 * (4 * j + wave) + (lane >> 2)) * rb + unit;
+        for (int j = 0; j < LX; ++j) off_x[j] = src(8 * (4 * j + wave) + (lane >> 3)) * rb + unit;
         off_sx = src(64 * wave + lane) * sb;
     };
     set_rows();
@@ -291,44 +517,56 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         static_cast<uint32_t>(wave) * 1024u;
     auto load_codes = [&](int j, int buf) {            // j < NL
         const uint32_t dst = lds_codes + static_cast<uint32_t>(buf) * (ROWS * kTlUnits * 16u);
-        if (j < LW) dma16(base_w + ls * 64, off_w[j], dst + static_cast<uint32_t>(j) * 4096u);
-        else dma16(base_x + ls * 64, off_x[j - LW], dst + kTlN * 64u + static_cast<uint32_t>(j - LW) * 4096u);
+        if (j < LW) mx4_copy16(base_w + ls * 128, off_w[j], dst + static_cast<uint32_t>(j) * 4096u);
+        else mx4_copy16(base_x + ls * 128, off_x[j - LW], dst + kTlN * 128u + static_cast<uint32_t>(j - LW) * 4096u);
     };
     uint32_t load_super = 0;               // byte offset of the cursor's scale buffer
-    auto load_scales = [&]() {             // before the loads of a stage that is 0 modulo 4
+    auto load_scales = [&]() {             // before the codes of an even pair
         const uint32_t dst = lds_scales + load_super;
-        dma16(base_sw + ls * 4, off_sw, dst);
-        if (BM == 256 || wave < BM / 64) dma16(base_sx + ls * 4, off_sx, dst + kTlN * 16u);
+        mx4_copy16(base_sw + ls * 8, off_sw, dst);
+        if (BM == 256 || wave < BM / 64) mx4_copy16(base_sx + ls * 8, off_sx, dst + kTlN * 16u);
         load_super ^= ROWS * 16u;
     };
 
     // ---- fragments
     u32x4 fw[2][IO], fx[XB];
-    int sw[IO], sx[IT], nsw[IO], nsx[IT];
-    const int frag0 = l16 * kTlUnits + (q ^ (l16 >> 2));
-    const u32x4* const rd_w = &codes[0][wo * 128 * kTlUnits + frag0];
-    const u32x4* const rd_x = &codes[0][(kTlN + wt * (BM / 2)) * kTlUnits + frag0];
-    auto read_w = [&](int i, int buf, int to) { fw[to][i] = rd_w[buf * (ROWS * kTlUnits) + i * 16 * kTlUnits]; };
-    auto read_x = [&](int j, int buf) { fx[j % XB] = rd_x[buf * (ROWS * kTlUnits) + j * 16 * kTlUnits]; };
-    // bytes q of a scale row's four dwords
-    const uint32_t pick = static_cast<uint32_t>(q) | (static_cast<uint32_t>(4 + q) << 8) | 0x0C0C0000u;
-    int read_super = 0;
-    auto gather = [&](u32x4 v) {
-        const uint32_t lo = __builtin_amdgcn_perm(v[1], v[0], pick);
-        const uint32_t hi = __builtin_amdgcn_perm(v[3], v[2], pick);
-        return static_cast<int>(lo | (hi << 16));
+    int sw[IO], sx[IT];
+    // lane (l16, q) reads row l16, unit 4 (stage % 2) + q
+    const int at0 = l16 * kTlUnits + (q ^ (l16 >> 1)), at1 = at0 ^ 4;
+    const u32x4* const rd_w = &codes[0][wo * 128 * kTlUnits];
+    const u32x4* const rd_x = &codes[0][(kTlN + wt * (BM / 2)) * kTlUnits];
+    auto frag_at = [&](int st, int i) {    // stage 0 .. 3: pair st / 2, half st % 2
+        return (st / 2) * (ROWS * kTlUnits) + i * 16 * kTlUnits + (st % 2 ? at1 : at0);
     };
-    const u32x4* const rd_sw = &scales[0][wo * 128 + l16];
-    const u32x4* const rd_sx = &scales[0][kTlN + wt * (BM / 2) + l16];
-    auto read_sw = [&](int i) { nsw[i] = gather(rd_sw[read_super + 16 * i]); };
-    auto read_sx = [&](int j) { nsx[j] = gather(rd_sx[read_super + 16 * j]); };
-    auto take_scales = [&]() {
-#pragma unroll
-        for (int i = 0; i < IO; ++i) sw[i] = nsw[i];
-#pragma unroll
-        for (int j = 0; j < IT; ++j) sx[j] = nsx[j];
-        read_super ^= ROWS;
+    auto read_w = [&](int i, int st) { fw[st % 2][i] = rd_w[frag_at(st, i)]; };
+    auto read_x = [&](int j, int st) { fx[j % XB] = rd_x[frag_at(st, j)]; };
+    // Scale bytes: the lane that copied a row's 16 bytes (byte 4 s + q for
+    // stage s, block column q) turns them in place into four dwords by q, byte
+    // s for stage s, once they have arrived.  A fragment's dword then needs no
+    // arithmetic: a vector instruction's result may be read by a matrix
+    // instruction only two wait states later, and the compiler does not see
+    // the ones written as text.
+    uint32_t turn_super = 0;
+    auto turn = [&](u32x4* p) {
+        const u32x4 v = *p;
+        const uint32_t a0 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u);    // 00 10 01 11
+        const uint32_t a1 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602u);    // 02 12 03 13
+        const uint32_t b0 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u);
+        const uint32_t b1 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602u);
+        *p = u32x4{__builtin_amdgcn_perm(b0, a0, 0x05040100u), __builtin_amdgcn_perm(b0, a0, 0x07060302u),
+                   __builtin_amdgcn_perm(b1, a1, 0x05040100u), __builtin_amdgcn_perm(b1, a1, 0x07060302u)};
     };
+    auto turn_scales = [&]() {
+        u32x4* const p = &scales[0][turn_super + 64 * wave + lane];
+        turn(p);
+        if (BM == 256 || wave < BM / 64) turn(p + kTlN);
+        turn_super ^= ROWS;
+    };
+    const int* const rd_sw = reinterpret_cast<const int*>(&scales[0][wo * 128 + l16]) + q;
+    const int* const rd_sx = reinterpret_cast<const int*>(&scales[0][kTlN + wt * (BM / 2) + l16]) + q;
+    uint32_t read_super = 0;
+    auto read_sw = [&](int i) { sw[i] = rd_sw[read_super + 64 * i]; };
+    auto read_sx = [&](int j) { sx[j] = rd_sx[read_super + 64 * j]; };
 
     f32x4 acc[IO][IT];
     auto clear = [&]() {
@@ -338,55 +576,86 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
             for (int j = 0; j < IT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     };
 
-    // accumulator (i, j): outputs 128 wo + 16 i + 4 q + e, row (BM/2) wt + 16 j + l16
+    // Accumulator (i, j) holds outputs 128 wo + 16 i + 4 q + e of row (BM/2) wt
+    // + 16 j + l16.  Sixteen rows at a time pass through LDS of the wave's own
+    // (16-byte unit u of row r at u ^ r), so that 16 lanes store 256
+    // contiguous bytes of a row: stored from the accumulators, pieces of 32
+    // bytes, a prefill's y took 68 us of 289.
+    auto sum = [&](int i, int j, int e) {
+        // read in place: as an ordinary value all 256 would change registers
+        float v;
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[i][j][e]));
+        return v;
+    };
+    u32x4* const out_lds = &outs[wave][0];
     auto store = [&](const Tile& t) {
+        // the last matrix step's result takes up to 18 wait states
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+        constexpr int PER = 16 / sizeof(Y);            // outputs of a unit
+        constexpr int PARTS = sizeof(Y) == 4 ? 2 : 1;  // 256-byte pieces of a wave's row
         const int rows = t.end - t.first, cols = a.d_out - t.n0;
-        const bool vec = (a.d_out & 3) == 0;
+        const bool vec = a.d_out % PER == 0;
 #pragma unroll
         for (int j = 0; j < IT; ++j) {
-            const int row = wt * (BM / 2) + 16 * j + l16;
-            if (row >= rows) continue;
-            Y* y = static_cast<Y*>(a.y) + static_cast<int64_t>(t.first + row) * a.d_out + t.n0;
 #pragma unroll
-            for (int i = 0; i < IO; ++i) {
-                const int c = wo * 128 + 16 * i + 4 * q;
-                const f32x4 v = acc[i][j];
-                if (vec) {
-                    if (c >= cols) continue;
-                    if constexpr (sizeof(Y) == 4) *reinterpret_cast<f32x4*>(y + c) = v;
-                    else *reinterpret_cast<u32x2*>(y + c) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-                } else {
+            for (int h = 0; h < PARTS; ++h) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c + e < cols) mx4_store(y + c + e, v[e]);
+                for (int ii = 0; ii < IO / PARTS; ++ii) {
+                    const int i = h * (IO / PARTS) + ii;
+                    const float v0 = sum(i, j, 0), v1 = sum(i, j, 1), v2 = sum(i, j, 2), v3 = sum(i, j, 3);
+                    if constexpr (sizeof(Y) == 4) {
+                        out_lds[l16 * 16 + ((4 * ii + q) ^ l16)] =
+                            u32x4{__float_as_uint(v0), __float_as_uint(v1), __float_as_uint(v2), __float_as_uint(v3)};
+                    } else {
+                        reinterpret_cast<u32x2*>(&out_lds[l16 * 16 + ((2 * ii + (q >> 1)) ^ l16)])[q & 1] =
+                            u32x2{pack_bf16(v0, v1), pack_bf16(v2, v3)};
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int lr = 4 * r + q;          // 16 lanes a row
+                    const u32x4 v = out_lds[lr * 16 + (l16 ^ lr)];
+                    const int row = wt * (BM / 2) + 16 * j + lr;
+                    const int c = wo * 128 + h * (128 / PARTS) + l16 * PER;
+                    if (row >= rows || c >= cols) continue;
+                    Y* y = static_cast<Y*>(a.y) + static_cast<int64_t>(t.first + row) * a.d_out + t.n0 + c;
+                    if (vec) {
+                        *reinterpret_cast<u32x4*>(y) = v;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < PER; ++e) {
+                            if (c + e >= cols) continue;
+                            if constexpr (sizeof(Y) == 4) y[e] = __uint_as_float(v[e]);
+                            else y[e] = static_cast<uint16_t>(v[e / 2] >> (16 * (e % 2)));
+                        }
+                    }
                 }
             }
         }
     };
 
-    // The sums are read by other instructions only behind this: the last
-    // matrix step's result takes up to 18 wait states.
-    auto settle = [&]() {
-        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < IO; ++i)
-#pragma unroll
-            for (int j = 0; j < IT; ++j) asm volatile("" : "+a"(acc[i][j]));
-    };
+    // The barrier of a stage comes behind row IT - 4 of its matrix steps; the
+    // AFTER steps that follow it are where the next stage's first fragments
+    // are read.  Copy c of a pair is issued SP c steps behind the barrier of a
+    // second stage, the last ones in the stage after it.
+    constexpr int BAR = (IT - 3) * IO - 1, AFTER = NM - 1 - BAR, SP = IT / 2;
+    constexpr int BEGUN = AFTER / SP + 1;  // copies issued before that stage ends
+    static_assert((NL - 1) * SP < AFTER + BAR, "copies are issued before the scales are waited for");
 
-    // ---- prologue: stages 0, 1 and 2 (nk >= 4)
+    // ---- prologue: pair 0 and the begun part of pair 1 (np >= 2)
     load_scales();
 #pragma unroll
-    for (int b = 0; b < 3; ++b) {
+    for (int j = 0; j < NL; ++j) load_codes(j, 0);
+    ls = 1;
 #pragma unroll
-        for (int j = 0; j < NL; ++j) load_codes(j, b);
-        ++ls;
-    }
-    wait_vmcnt<2 * NL>();
+    for (int j = 0; j < BEGUN; ++j) load_codes(j, 1);
+    wait_vmcnt<BEGUN>();
+    asm volatile("" ::: "memory");
+    turn_scales();
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < IO; ++i) {
-        read_w(i, 0, 0);
+        read_w(i, 0);
         read_sw(i);
     }
 #pragma unroll
@@ -395,48 +664,66 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     for (int j = 0; j < XB - 1; ++j) read_x(j, 0);
     clear();
 
-    for (int64_t k = 0;;) {
-        for (int kt = 0; kt < nk; kt += 4) {
-            take_scales();
-#define CAT_STAGE(B)                                                                             \
-    {                                                                                            \
-        constexpr int L = (B + 3) % 4;                                                           \
-        wait_vmcnt<NL + (B == 2 ? (BM == 256 ? 2 : 1) : 0)>();                                   \
-        lds_barrier();                                                                           \
-        if (L == 0) load_scales();                                                               \
-        _Pragma("unroll") for (int m = 0; m < NM; ++m) {                                         \
-            const int j = m / IO, i = m % IO;                                                    \
-            mx4_mfma_acc<B>(fw[B & 1][i], fx[j % XB], acc[i][j], sw[i], sx[j]);                  \
-            if (m % 4 == 1 && m / 4 < NL) load_codes(m / 4, L);                           \
-            if (i == 0) {                                                                        \
-                if (j + XB - 1 < IT) read_x(j + XB - 1, B);                                      \
-                else read_x(j + XB - 1 - IT, (B + 1) % 4);                                       \
-            }                                                                                    \
-            if (m % (NM / IO) == NM / IO / 2) read_w(m / (NM / IO), (B + 1) % 4, (B + 1) & 1);   \
-            if (B == 3 && i == 2) {                                                              \
-                read_sx(j);                                                                      \
-                if (IT == 8) read_sw(j);                                                         \
-                else read_sw(2 * j), read_sw(2 * j + 1);                                         \
-            }                                                                                    \
-        }                                                                                        \
-        ++ls;                                                                                    \
-        if (L == 3 && ls == nk) {                                                                \
-            ls = 0;                                                                              \
-            if (tile_at(++lk, lt)) set_rows();                                                   \
-        }                                                                                        \
-    }
-            CAT_STAGE(0)
-            CAT_STAGE(1)
-            CAT_STAGE(2)
-            CAT_STAGE(3)
-#undef CAT_STAGE
+    auto copy_at = [&](int steps, int buf) {   // copies due `steps` behind the barrier
+        if (steps % SP == 0 && steps / SP < NL) load_codes(steps / SP, buf);
+    };
+    auto stage = [&](auto st_) {
+        constexpr int B = decltype(st_)::value, N = (B + 1) % 4;
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            const int j = m / IO, i = m % IO;
+            mx4_mfma_acc<B>(fw[B % 2][i], fx[j % XB], acc[i][j], sw[i], sx[j]);
+            if (i == 0 && j + XB - 1 < IT) read_x(j + XB - 1, B);
+            if (m == BAR) {
+                if (B % 2 == 1) {
+                    wait_vmcnt<0>();
+                    lds_barrier();
+                    if (B == 1) load_scales();
+                } else if (B == 2) {
+                    wait_vmcnt<NL>();
+                    asm volatile("" ::: "memory");
+                    turn_scales();
+                }
+                if (B == 3) {
+                    read_super ^= 4 * ROWS;
+#pragma unroll
+                    for (int e = 0; e <= j; ++e) read_sx(e);
+                }
+            }
+            // copies: into buffer 0 behind stage 1's barrier, 1 behind stage 3's
+            if (B % 2 == 1 && m >= BAR) copy_at(m - BAR, B / 2);
+            if (B % 2 == 0) copy_at(m + 1 + AFTER, N == 3 ? 0 : 1);
+            // next stage's fragments: of another pair only behind the barrier
+            if (i == 0 && j + XB - 1 >= IT) read_x(j + XB - 1 - IT, N);
+            if (B % 2 == 1) {
+                if (m > BAR && (m - BAR) % 3 == 2 && (m - BAR) / 3 < IO) read_w((m - BAR) / 3, N);
+            } else if (m % (NM / IO) == NM / IO / 2) {
+                read_w(m / (NM / IO), N);
+            }
+            // the next two pairs' scales, each behind its last use
+            if (B == 3 && i == IO - 1 && m > BAR) read_sx(j);
+            if (B == 3 && j == IT - 1) read_sw(i);
         }
-        settle();
+        if (B % 2 == 0) {
+            ++ls;
+            if (B == 0 && ls == np) {      // after an odd pair only
+                ls = 0;
+                if (tile_at(++lk, lt)) set_rows();
+            }
+        }
+    };
+    for (int64_t k = 0;;) {
+        for (int p = 0; p < np; p += 2) {
+            stage(std::integral_constant<int, 0>{});
+            stage(std::integral_constant<int, 1>{});
+            stage(std::integral_constant<int, 2>{});
+            stage(std::integral_constant<int, 3>{});
+        }
         store(tile);
         if (!tile_at(++k, tile)) break;
         clear();
     }
-    wait_vmcnt<0>();                       // the requests past the last stage
+    wait_vmcnt<0>();                       // the requests past the last pair
 }
 
 // Large tiles need whole pairs of stages (scale rows of whole 16 bytes) and
@@ -458,13 +745,42 @@ static hipError_t launch_tiles(const Mx4Args& a, int y_bf16, hipStream_t stream)
     return hipGetLastError();
 }
 
-static hipError_t launch(const Mx4Args& a, int y_bf16, hipStream_t stream) {
-    if (tile_fits(a) && a.m >= 256) return launch_tiles<256>(a, y_bf16, stream);
-    const int64_t row_tiles = (a.m + 15) / 16 + (a.offsets ? a.groups : 0);
-    const dim3 grid(static_cast<unsigned>(row_tiles), static_cast<unsigned>((a.d_out + 15) / 16));
-    if (y_bf16) mx4_gemm_kernel<uint16_t><<<grid, kWave, 0, stream>>>(a);
-    else mx4_gemm_kernel<float><<<grid, kWave, 0, stream>>>(a);
+// Tile shapes of the split kernel: rows / 16, outputs / 16, ring chunks.
+struct SpTile {
+    int a, b;
+};
+#define CAT_SPLIT_TILES(V) \
+    V(0, 1, 1, 4) V(1, 1, 2, 4) V(2, 1, 4, 3) V(3, 2, 2, 4) V(4, 2, 4, 2) V(5, 3, 4, 2) V(6, 5, 4, 2) V(7, 4, 4, 2)
+#define CAT_SPLIT_AB(id, A, B, D) {A, B},
+static constexpr SpTile kSpTiles[] = {CAT_SPLIT_TILES(CAT_SPLIT_AB)};
+#undef CAT_SPLIT_AB
+// A launch covers fewer than 2^32 threads; workgroups then take several tiles.
+constexpr int64_t kSpMaxGrid = int64_t{1} << 22;
+constexpr int kSpTileCount = sizeof(kSpTiles) / sizeof(kSpTiles[0]);
+
+template <typename Y, bool ALN>
+static hipError_t launch_split(const Mx4Args& a, int tile, hipStream_t stream) {
+    const SpTile& t = kSpTiles[tile];
+    const int64_t T = mx4_row_tiles_most(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
+    const int64_t wgs = (T + kMxXcd - 1) / kMxXcd * kMxXcd;
+    const dim3 grid(static_cast<unsigned>(wgs < kSpMaxGrid ? wgs : kSpMaxGrid));
+    switch (tile) {
+#define CAT_SPLIT_CASE(id, A, B, D) \
+    case id: mx4_split_kernel<Y, A, B, sp_depth(A, B, D, ALN), ALN><<<grid, kSpThreads, 0, stream>>>(a); break;
+        CAT_SPLIT_TILES(CAT_SPLIT_CASE)
+#undef CAT_SPLIT_CASE
+        default: return hipErrorInvalidValue;
+    }
     return hipGetLastError();
+}
+
+static hipError_t launch(const Mx4Args& a, int y_bf16, hipStream_t stream) {
+    int tile = a.m > 64 ? 7 : a.m > 32 ? 5 : a.m > 16 ? 3 : 0;
+    if (a.m >= 256 && tile_fits(a)) tile = kSpTileCount;
+    if (tile == kSpTileCount) return launch_tiles<256>(a, y_bf16, stream);
+    if (a.d_in % 128 == 0)
+        return y_bf16 ? launch_split<uint16_t, true>(a, tile, stream) : launch_split<float, true>(a, tile, stream);
+    return y_bf16 ? launch_split<uint16_t, false>(a, tile, stream) : launch_split<float, false>(a, tile, stream);
 }
 
 hipError_t launch_mx4_linear(const uint8_t* cx, const uint8_t* ex, const uint8_t* cw,
