@@ -185,6 +185,18 @@ def _torch():
     return _torch_module
 
 
+_dtype_sets = {}
+
+
+def _types(name):
+    """The dtypes an operand may have, as one tuple kept per set."""
+    if not _dtype_sets:
+        torch = _torch()
+        _dtype_sets.update(u8=(torch.uint8,), i8=(torch.int8,), i32=(torch.int32,),
+                           f32=(torch.float32,), float=(torch.bfloat16, torch.float32))
+    return _dtype_sets[name]
+
+
 def _dev_ptr(t, name, dtypes=None, allow_none=False):
     # A decode step's kernels run for a few microseconds, so the marshalling
     # is what a small call costs: the passing case takes four attribute reads
@@ -212,6 +224,8 @@ def _shape(t, shape, name):
     """The C ABI takes bare pointers and cannot see buffer sizes, so every
     buffer's shape is checked here, before the call: a short buffer would
     otherwise be read or written past its end on the device."""
+    if t.shape == shape:        # the passing case of a tuple: 0.1 us
+        return
     if tuple(t.shape) != tuple(int(v) for v in shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
@@ -527,23 +541,21 @@ def cat_full_hadamard_weights(W_prime, k: int):
 def _one_device(stream, first, *others):
     """Every tensor on one device, and that device the current one: kernels
     are launched there, on the current stream or on `stream`."""
-    dev = first.device
+    dev = first.get_device()
     for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
-    torch = _torch()
-    current = _current_device() if _current_device is not None else torch.cuda.current_device()
-    if dev.index != current:
-        raise ValueError(f"tensors on {dev}, but the current device is cuda:{current}")
-    if stream is not None and stream.device != dev:
-        raise ValueError(f"tensors on {dev}, stream on {stream.device}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on different devices: cuda:{dev} and {t.device}")
+    current = _current_device() if _current_device is not None else _torch().cuda.current_device()
+    if dev != current:
+        raise ValueError(f"tensors on cuda:{dev}, but the current device is cuda:{current}")
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"tensors on cuda:{dev}, stream on cuda:{stream.device_index}")
 
 
 def _rmsnorm_args(x, weight, codes, scales, residual, residual_out, stream):
     """Checks shared by the RMS norm calls; (n, d, pointers of x, residual,
     residual_out and weight)."""
-    torch = _torch()
-    floats = (torch.bfloat16, torch.float32)
+    floats = _types("float")
     px = _dev_ptr(x, "x", floats)
     pw = _dev_ptr(weight, "weight", floats)
     if x.dim() != 2:
@@ -566,9 +578,8 @@ def cat_rmsnorm_quant(x, weight, codes, s_x, residual=None, residual_out=None, e
     """codes int8 [n, d] and s_x [n] fp32 of the RMS norm of h = x +
     residual times weight [d]; residual_out (which may be residual or x)
     receives h in x's dtype.  x, residual [n, d] bf16 or fp32."""
-    torch = _torch()
-    pc = _dev_ptr(codes, "codes", (torch.int8,))
-    ps = _dev_ptr(s_x, "s_x", (torch.float32,))
+    pc = _dev_ptr(codes, "codes", _types("i8"))
+    ps = _dev_ptr(s_x, "s_x", _types("f32"))
     n, d, px, pr, po, pw = _rmsnorm_args(x, weight, codes, s_x, residual, residual_out, stream)
     _shape(codes, (n, d), "codes")
     _numel(s_x, n, "s_x")
@@ -581,9 +592,8 @@ def cat_rmsnorm_mx4(x, weight, codes, scales, residual=None, residual_out=None, 
                     stream=None):
     """cat_rmsnorm_quant with MXFP4 output: codes uint8 [n, d/2] and scales
     uint8 [n, d/32]."""
-    torch = _torch()
-    pc = _dev_ptr(codes, "codes", (torch.uint8,))
-    ps = _dev_ptr(scales, "scales", (torch.uint8,))
+    pc = _dev_ptr(codes, "codes", _types("u8"))
+    ps = _dev_ptr(scales, "scales", _types("u8"))
     n, d, px, pr, po, pw = _rmsnorm_args(x, weight, codes, scales, residual, residual_out, stream)
     _mx4_shapes(codes, scales, (n,), d)
     _check("cat_rmsnorm_mx4",
@@ -591,20 +601,21 @@ def cat_rmsnorm_mx4(x, weight, codes, scales, residual=None, residual_out=None, 
                                  pc, ps, _stream_ptr(stream)))
 
 
-def _mx4_shapes(codes, scales, lead, d, names=("codes", "scales")):
+def _mx4_shapes(codes, scales, lead, d, codes_name="codes", scales_name="scales"):
+    if d % 32 == 0 and codes.shape == (*lead, d >> 1) and scales.shape == (*lead, d >> 5):
+        return
     if d % 32:
         raise ValueError(f"rows of {d} elements are not whole blocks of 32")
-    _shape(codes, (*lead, d // 2), names[0])
-    _shape(scales, (*lead, d // 32), names[1])
+    _shape(codes, (*lead, d // 2), codes_name)
+    _shape(scales, (*lead, d // 32), scales_name)
 
 
 def cat_mx4_quant(X, codes, scales, stream=None):
     """MXFP4 codes uint8 [n, d/2] and scales uint8 [n, d/32] of X [n, d]
     (bf16 or fp32; activations or weights)."""
-    torch = _torch()
-    px = _dev_ptr(X, "X", (torch.bfloat16, torch.float32))
-    pc = _dev_ptr(codes, "codes", (torch.uint8,))
-    ps = _dev_ptr(scales, "scales", (torch.uint8,))
+    px = _dev_ptr(X, "X", _types("float"))
+    pc = _dev_ptr(codes, "codes", _types("u8"))
+    ps = _dev_ptr(scales, "scales", _types("u8"))
     if X.dim() != 2:
         raise ValueError("X must be [n, d]")
     n, d = X.shape
@@ -616,10 +627,9 @@ def cat_mx4_quant(X, codes, scales, stream=None):
 
 def cat_mx4_dequant(codes, scales, out, stream=None):
     """out [n, d] (bf16 or fp32): the values of MXFP4 codes and scales."""
-    torch = _torch()
-    pc = _dev_ptr(codes, "codes", (torch.uint8,))
-    ps = _dev_ptr(scales, "scales", (torch.uint8,))
-    po = _dev_ptr(out, "out", (torch.bfloat16, torch.float32))
+    pc = _dev_ptr(codes, "codes", _types("u8"))
+    ps = _dev_ptr(scales, "scales", _types("u8"))
+    po = _dev_ptr(out, "out", _types("float"))
     if out.dim() != 2:
         raise ValueError("out must be [n, d]")
     n, d = out.shape
@@ -632,19 +642,18 @@ def cat_mx4_dequant(codes, scales, out, stream=None):
 def cat_mx4_linear(codes_x, scales_x, codes_w, scales_w, y, stream=None):
     """y [n, d_out] (bf16 or fp32) = x w^T of MXFP4 codes_x [n, d_in/2] and
     codes_w [d_out, d_in/2] with their scales [.., d_in/32]."""
-    torch = _torch()
-    u8 = (torch.uint8,)
+    u8 = _types("u8")
     pcx = _dev_ptr(codes_x, "codes_x", u8)
     psx = _dev_ptr(scales_x, "scales_x", u8)
     pcw = _dev_ptr(codes_w, "codes_w", u8)
     psw = _dev_ptr(scales_w, "scales_w", u8)
-    py = _dev_ptr(y, "y", (torch.bfloat16, torch.float32))
+    py = _dev_ptr(y, "y", _types("float"))
     if codes_x.dim() != 2 or codes_w.dim() != 2:
         raise ValueError("codes_x and codes_w must be 2-D")
     n, half = codes_x.shape
     d_out = codes_w.shape[0]
-    _mx4_shapes(codes_x, scales_x, (n,), 2 * half, ("codes_x", "scales_x"))
-    _mx4_shapes(codes_w, scales_w, (d_out,), 2 * half, ("codes_w", "scales_w"))
+    _mx4_shapes(codes_x, scales_x, (n,), 2 * half, "codes_x", "scales_x")
+    _mx4_shapes(codes_w, scales_w, (d_out,), 2 * half, "codes_w", "scales_w")
     _shape(y, (n, d_out), "y")
     _one_device(stream, codes_x, scales_x, codes_w, scales_w, y)
     _check("cat_mx4_linear",
@@ -658,22 +667,21 @@ def cat_mx4_linear_grouped(codes_x, scales_x, offsets, codes_w, scales_w, y, row
     1] (int32 [groups + 1]) times the weights codes_w[g] of [groups, d_out,
     d_in/2].  Row i of y takes row i of codes_x [n, d_in/2], n >= m, or row
     row_ids[i] (int32 [m])."""
-    torch = _torch()
-    u8 = (torch.uint8,)
+    u8 = _types("u8")
     pcx = _dev_ptr(codes_x, "codes_x", u8)
     psx = _dev_ptr(scales_x, "scales_x", u8)
-    pof = _dev_ptr(offsets, "offsets", (torch.int32,))
+    pof = _dev_ptr(offsets, "offsets", _types("i32"))
     pcw = _dev_ptr(codes_w, "codes_w", u8)
     psw = _dev_ptr(scales_w, "scales_w", u8)
-    pid = _dev_ptr(row_ids, "row_ids", (torch.int32,), allow_none=True)
-    py = _dev_ptr(y, "y", (torch.bfloat16, torch.float32))
+    pid = _dev_ptr(row_ids, "row_ids", _types("i32"), allow_none=True)
+    py = _dev_ptr(y, "y", _types("float"))
     if codes_x.dim() != 2 or codes_w.dim() != 3 or y.dim() != 2:
         raise ValueError("codes_x and y must be 2-D, codes_w 3-D")
     n, half = codes_x.shape
     groups, d_out, _ = codes_w.shape
     m = y.shape[0]
-    _mx4_shapes(codes_x, scales_x, (n,), 2 * half, ("codes_x", "scales_x"))
-    _mx4_shapes(codes_w, scales_w, (groups, d_out), 2 * half, ("codes_w", "scales_w"))
+    _mx4_shapes(codes_x, scales_x, (n,), 2 * half, "codes_x", "scales_x")
+    _mx4_shapes(codes_w, scales_w, (groups, d_out), 2 * half, "codes_w", "scales_w")
     _shape(y, (m, d_out), "y")
     _numel(offsets, groups + 1, "offsets")
     if pid is not None:

@@ -3,6 +3,7 @@
 // on the block-scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4:
 // lane L holds row L % 16, elements [32 (L / 16), 32 (L / 16) + 32) of a
 // step of 128 (16 bytes of codes) and that block's scale byte.
+#include <cmath>
 #include <type_traits>
 
 #include "kernels.h"
@@ -94,36 +95,60 @@ __device__ __forceinline__ int mx4_source_row(const Mx4Args& a, int i) {
     return s < 0 ? 0 : (s < a.n ? s : a.n - 1);
 }
 
+__device__ __forceinline__ void mx4_store(float* y, float v) { *y = v; }
+__device__ __forceinline__ void mx4_store(uint16_t* y, float v) {
+    *y = static_cast<uint16_t>(pack_bf16(v, 0.0f));
+}
+
+// Four outputs of row `row` and column `col` of the tile at (first, n0), of
+// which rows x cols exist.
+template <typename Y>
+__device__ __forceinline__ void mx4_store4(Y* y, int d_out, int first, int n0, int rows, int cols,
+                                           int row, int col, f32x4 v) {
+    if (row >= rows || col >= cols) return;
+    y += static_cast<int64_t>(first + row) * d_out + n0 + col;
+    if ((d_out & 3) == 0) {
+        if constexpr (sizeof(Y) == 4) *reinterpret_cast<f32x4*>(y) = v;
+        else *reinterpret_cast<u32x2*>(y) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < cols) mx4_store(y + e, v[e]);
+    }
+}
+
 // global -> LDS copies as dma16 and dma4 of the common header (16 or 4 bytes a
 // lane, the lane's bytes at lds + 16 or 4 lane), with M0 given up instead of
-// saved: nothing else here keeps a value in it, and a copy is then three
-// instructions.  The first takes a wave-uniform base and a 32-bit offset a
-// lane, the others an address a lane.
+// saved: nothing else in these kernels uses it, and a copy is then three
+// instructions.  From a wave-uniform base and a 32-bit offset a lane, or from
+// an address a lane.
 __device__ __forceinline__ void mx4_copy16(const uint8_t* base, uint32_t off, uint32_t lds) {
     asm volatile(
         "s_mov_b32 m0, %2\n\t"
         "s_nop 0\n\t"
         "global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds)
-        : "memory", "m0");
+        : "memory");
+}
+__device__ __forceinline__ void mx4_copy4(const uint8_t* base, uint32_t off, uint32_t lds) {
+    asm volatile(
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds)
+        : "memory");
 }
 __device__ __forceinline__ void mx4_copy16(const uint8_t* p, uint32_t lds) {
     asm volatile(
         "s_mov_b32 m0, %1\n\t"
         "s_nop 0\n\t"
         "global_load_lds_dwordx4 %0, off" ::"v"(p), "s"(lds)
-        : "memory", "m0");
+        : "memory");
 }
 __device__ __forceinline__ void mx4_copy4(const uint8_t* p, uint32_t lds) {
     asm volatile(
         "s_mov_b32 m0, %1\n\t"
         "s_nop 0\n\t"
         "global_load_lds_dword %0, off" ::"v"(p), "s"(lds)
-        : "memory", "m0");
-}
-
-__device__ __forceinline__ void mx4_store(float* y, float v) { *y = v; }
-__device__ __forceinline__ void mx4_store(uint16_t* y, float v) {
-    *y = static_cast<uint16_t>(pack_bf16(v, 0.0f));
+        : "memory");
 }
 
 // -------------------------------------------------- tiles for fewer rows
@@ -151,10 +176,6 @@ constexpr int sp_stage_bytes(int a, int b, bool aligned) {
     return (a + b) * 1024 + (a + b + 3) / 4 * 256 * (aligned ? 1 : 2);
 }
 constexpr int sp_round(int a, int b) { return a * b < 8 ? a * b : 8; }
-// The ring's depth: D where it fits the LDS, else one less.
-constexpr int sp_depth(int a, int b, int d, bool aligned) {
-    return d * sp_stage_bytes(a, b, aligned) * kSpWaves <= 160 * 1024 ? d : d - 1;
-}
 constexpr int sp_wave_bytes(int a, int b, int d, bool aligned) {
     return d * sp_stage_bytes(a, b, aligned) > sp_round(a, b) * 1024 ? d * sp_stage_bytes(a, b, aligned)
                                                                      : sp_round(a, b) * 1024;
@@ -316,28 +337,221 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += p[e];
             }
-            const int row = (tl / B) * 16 + l16, col = (tl % B) * 16 + 4 * q;
-            if (row < rows_x && col < rows_w) {
-                Y* y = static_cast<Y*>(a.y) + static_cast<int64_t>(r.first + row) * a.d_out + n0 + col;
-                if ((a.d_out & 3) == 0) {
-                    if constexpr (sizeof(Y) == 4) *reinterpret_cast<f32x4*>(y) = v;
-                    else *reinterpret_cast<u32x2*>(y) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (col + e < rows_w) mx4_store(y + e, v[e]);
-                }
-            }
+            mx4_store4(static_cast<Y*>(a.y), a.d_out, r.first, n0, rows_x, rows_w, (tl / B) * 16 + l16,
+                       (tl % B) * 16 + 4 * q, v);
         }
     }
 }
 
-template <typename Y, int A, int B, int D, bool ALN>
-__global__ __launch_bounds__(kSpThreads) void mx4_split_kernel(Mx4Args a) {
+// The same with whole cache lines, for rows of at least 512 elements: a chunk
+// is 256 elements, 128 bytes of every row (8 rows a copy), and 16 bytes that
+// hold its 8 scale bytes (64 rows a copy).  Every copy costs a CU about the
+// same, and copies of whole lines reach almost twice the rate of 64-byte
+// pieces.  Wave w of W takes the w-th part of the chunks, in order.
+//
+// EX: d_in % 512 == 0, so that scale pieces are whole 16 bytes at multiples of
+// 16 of their row.  Otherwise a piece begins at the dword that holds its
+// chunk's first byte, moved back where it would pass the buffer's last dword,
+// and a lane finds its bytes in it; units past a row's end count as zero with
+// scale 1.
+constexpr int ln_stage_bytes(int a, int b) { return (2 * (a + b) + (a + b + 3) / 4) * 1024; }
+constexpr int ln_round(int a, int b, int w) { return a * b < w ? a * b : w; }
+constexpr int ln_wave_bytes(int a, int b, int d, int w) {
+    return d * ln_stage_bytes(a, b) > ln_round(a, b, w) * 1024 ? d * ln_stage_bytes(a, b)
+                                                               : ln_round(a, b, w) * 1024;
+}
+
+template <typename Y, int A, int B, int D, int W, bool EX>
+__device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r, int n0,
+                                              uint8_t (&lds)[W][ln_wave_bytes(A, B, D, W)]) {
     constexpr int BM = 16 * A, BN = 16 * B;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kSpWaves][sp_wave_bytes(A, B, D, ALN)];
-    // XCD x walks one contiguous range of tiles, the row tiles of a column
-    // panel next to each other: its weights then enter that XCD's L2 once
+    constexpr int L = A + B;
+    constexpr int SC = (L + 3) / 4;        // scale copies per chunk
+    constexpr int COPIES = 2 * L + SC;
+    static_assert(COPIES * (D - 1) < 64, "copies in flight must fit the vmcnt range");
+    constexpr int kScaleAt = 2 * L * 1024, kStageBytes = ln_stage_bytes(A, B);
+    constexpr int RT = ln_round(A, B, W);  // accumulators added per round
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int l16 = lane & 15, q = lane >> 4;
+    const uint32_t rb = static_cast<uint32_t>(a.d_in) / 2;
+    const uint32_t sb = static_cast<uint32_t>(a.d_in) / 32;
+    const int nk = (a.d_in + 255) / 256;
+    const int c0 = nk * wave / W, cnt = nk * (wave + 1) / W - c0;
+    const int rows_x = r.end - r.first < BM ? r.end - r.first : BM;
+    const int rows_w = a.d_out - n0 < BN ? a.d_out - n0 : BN;
+    const int64_t w0 = static_cast<int64_t>(r.group) * a.d_out + n0;
+    // rows past the end read the last one (their results are not stored)
+    auto x_row = [&](int i) {
+        return static_cast<int64_t>(mx4_source_row(a, r.first + (i < rows_x ? i : rows_x - 1)));
+    };
+    auto w_row = [&](int o) { return o < rows_w ? o : rows_w - 1; };
+
+    // copy 2 f + h of a chunk: rows 8 h .. 8 h + 7 of fragment f, unit u of row
+    // r at slot 8 r + (u ^ (r >> 1))
+    const int cr = lane >> 3;
+    const uint32_t cu = 16u * static_cast<uint32_t>((lane & 7) ^ (lane >> 4));
+    const uint8_t* src_x[2 * A];
+    uint32_t src_w[2 * B];
+#pragma unroll
+    for (int g = 0; g < 2 * A; ++g) src_x[g] = a.cx + x_row(8 * g + cr) * rb;
+#pragma unroll
+    for (int g = 0; g < 2 * B; ++g) src_w[g] = static_cast<uint32_t>(w_row(8 * g + cr)) * rb;
+    const uint8_t* const base_w = a.cw + w0 * rb;
+    // A scale row by its byte address; the last place where 16 bytes may be
+    // read from its buffer.
+    auto scale_row = [&](int i) {          // tokens, then weights
+        return reinterpret_cast<uint64_t>(i < BM ? a.ex + x_row(i) * sb : a.ew + (w0 + w_row(i - BM)) * sb);
+    };
+    auto scale_most = [&](int i) {
+        const uint64_t first = reinterpret_cast<uint64_t>(i < BM ? a.ex : a.ew);
+        const int64_t bytes = (i < BM ? static_cast<int64_t>(a.n) : static_cast<int64_t>(a.groups) * a.d_out) * sb;
+        return first + static_cast<uint64_t>((bytes - 1) & ~int64_t{3}) - 12;
+    };
+    uint64_t ssrc[SC], smost[SC];          // of row 64 g + lane
+#pragma unroll
+    for (int g = 0; g < SC; ++g) {
+        const int i = 64 * g + lane < 16 * L ? 64 * g + lane : 16 * L - 1;
+        ssrc[g] = scale_row(i);
+        if (!EX) {
+            ssrc[g] &= ~uint64_t{3};
+            smost[g] = scale_most(i);
+        }
+    }
+    const uint32_t ring = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds_addr(&lds[wave][0])));
+    auto issue = [&](int i, int st) {      // the wave's i-th chunk
+        const uint32_t at = ring + static_cast<uint32_t>(st * kStageBytes);
+        const int c = c0 + i;
+#pragma unroll
+        for (int g = 0; g < SC; ++g) {
+            uint64_t p = ssrc[g] + static_cast<uint32_t>(EX ? (c >> 1) * 16 : c * 8);
+            if (!EX) p = p < smost[g] ? p : smost[g];
+            mx4_copy16(reinterpret_cast<const uint8_t*>(p), at + kScaleAt + g * 1024u);
+        }
+        uint32_t col[2];                   // of even and odd copies
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            col[h] = static_cast<uint32_t>(c) * 128u + (cu ^ (64u * h));
+            if (!EX) col[h] = col[h] < rb ? col[h] : 0;        // past the row's end: any unit of it
+        }
+#pragma unroll
+        for (int g = 0; g < 2 * B; ++g) mx4_copy16(base_w, src_w[g] + col[g & 1], at + (2 * A + g) * 1024u);
+#pragma unroll
+        for (int g = 0; g < 2 * A; ++g) mx4_copy16(src_x[g] + col[g & 1], at + g * 1024u);
+    };
+    const int at0 = 16 * (8 * l16 + (q ^ (l16 >> 1))), at1 = at0 ^ 64;
+    // general rows: a lane's scale byte of chunk c lies 8 c - max(8 c, far)
+    // before byte `near` of its row's piece
+    int near[EX ? 1 : L], far[EX ? 1 : L];
+    if (!EX) {
+#pragma unroll
+        for (int g = 0; g < L; ++g) {
+            const uint64_t row = scale_row(16 * g + l16);
+            const int64_t left = static_cast<int64_t>(scale_most(16 * g + l16) - (row & ~uint64_t{3}));
+            near[g] = static_cast<int>(row & 3) + q;
+            far[g] = static_cast<int>(left < (1 << 30) ? left : (1 << 30));
+        }
+    }
+    u32x4 f[2][L];
+    int s[2][L];
+    auto read = [&](int i, int st) {
+        const uint8_t* at = &lds[wave][st * kStageBytes];
+        const uint8_t* sc = at + kScaleAt + 16 * l16;
+        const int c = c0 + i;
+        if (EX) sc += q + 8 * (c & 1);
+#pragma unroll
+        for (int g = 0; g < L; ++g) {
+            const uint8_t* p = sc + 256 * g;
+            int i0 = 0, i1 = 4;
+            if (!EX) {                     // bytes past the row's end: any of the piece
+                const int at_byte = near[g] + (8 * c > far[g] ? 8 * c - far[g] : 0);
+                i0 = at_byte & 15;
+                i1 = (at_byte + 4) & 15;
+            }
+            s[0][g] = p[i0];
+            s[1][g] = p[i1];
+            f[0][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at0);
+            f[1][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at1);
+        }
+        if (!EX && c == nk - 1) {          // units past the row's end
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool past = 8 * c + 4 * h + q >= static_cast<int>(sb);
+#pragma unroll
+                for (int g = 0; g < L; ++g) {
+                    s[h][g] = past ? kMxByteOne : s[h][g];
+                    f[h][g] = past ? u32x4{0u, 0u, 0u, 0u} : f[h][g];
+                }
+            }
+        }
+    };
+    f32x4 acc[A][B];
+#pragma unroll
+    for (int i = 0; i < A; ++i)
+#pragma unroll
+        for (int j = 0; j < B; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto compute = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < A; ++i)
+#pragma unroll
+                for (int j = 0; j < B; ++j)
+                    acc[i][j] = mx4_mfma(f[h][A + j], f[h][i], acc[i][j], s[h][A + j], s[h][i]);
+    };
+#pragma unroll
+    for (int st = 0; st < D; ++st)
+        if (st < cnt) issue(st, st);
+    int i = 0, st = 0;
+    for (; i + D < cnt; ++i) {
+        wait_vmcnt<(D - 1) * COPIES>();
+        asm volatile("" ::: "memory");
+        read(i, st);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        issue(i + D, st);
+        compute();
+        st = st + 1 == D ? 0 : st + 1;
+    }
+    wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+    for (; i < cnt; ++i) {
+        read(i, st);
+        compute();
+        st = st + 1 == D ? 0 : st + 1;
+    }
+
+    // partial sums, RT accumulators a round: lane holds row l16, outputs 4 q .. + 3
+    constexpr int ROUNDS = (A * B + RT - 1) / RT;
+#pragma unroll
+    for (int rd = 0; rd < ROUNDS; ++rd) {
+        __syncthreads();                   // the ring (or the last round) is read
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int tl = rd * RT + t;
+            if (tl < A * B)
+                reinterpret_cast<f32x4*>(&lds[wave][0])[t * kWave + lane] = acc[tl / B][tl % B];
+        }
+        __syncthreads();
+        const int tl = rd * RT + wave;
+        if (wave < RT && tl < A * B) {
+            f32x4 v = reinterpret_cast<const f32x4*>(&lds[0][0])[wave * kWave + lane];
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                const f32x4 p = reinterpret_cast<const f32x4*>(&lds[w][0])[wave * kWave + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += p[e];
+            }
+            mx4_store4(static_cast<Y*>(a.y), a.d_out, r.first, n0, rows_x, rows_w, (tl / B) * 16 + l16,
+                       (tl % B) * 16 + 4 * q, v);
+        }
+    }
+}
+
+// Tiles of the call, walked so that XCD x (workgroups are dealt to the 8 of
+// them in turn) takes one contiguous range, the row tiles of a column panel
+// next to each other: its weights then enter that XCD's L2 once.
+template <int BM, int BN, typename F>
+__device__ __forceinline__ void mx4_walk(const Mx4Args& a, F tile) {
     const int tiles_n = (a.d_out + BN - 1) / BN;
     const int64_t row_tiles = mx4_row_tiles_most(a, BM);
     const int64_t T = row_tiles * tiles_n;
@@ -351,9 +565,21 @@ __global__ __launch_bounds__(kSpThreads) void mx4_split_kernel(Mx4Args a) {
         r.group = __builtin_amdgcn_readfirstlane(r.group);
         r.first = __builtin_amdgcn_readfirstlane(r.first);
         r.end = __builtin_amdgcn_readfirstlane(r.end);
-        mx4_split_tile<Y, A, B, D, ALN>(a, r, tn * BN, lds);
+        tile(r, tn * BN);
         __syncthreads();                   // the sums are read before the next ring
     }
+}
+
+template <typename Y, int A, int B, int D, bool ALN>
+__global__ __launch_bounds__(kSpThreads) void mx4_split_kernel(Mx4Args a) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kSpWaves][sp_wave_bytes(A, B, D, ALN)];
+    mx4_walk<16 * A, 16 * B>(a, [&](const Mx4Rows& r, int n0) { mx4_split_tile<Y, A, B, D, ALN>(a, r, n0, lds); });
+}
+
+template <typename Y, int A, int B, int D, int W, bool EX>
+__global__ __launch_bounds__(W * kWave) void mx4_line_kernel(Mx4Args a) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[W][ln_wave_bytes(A, B, D, W)];
+    mx4_walk<16 * A, 16 * B>(a, [&](const Mx4Rows& r, int n0) { mx4_line_tile<Y, A, B, D, W, EX>(a, r, n0, lds); });
 }
 
 // ------------------------------------------------------------- large tiles
@@ -424,7 +650,7 @@ __device__ __forceinline__ void mx4_mfma_acc(u32x4 a, u32x4 b, f32x4& acc, int s
 #undef CAT_MFMA
 }
 
-template <typename Y, int BM>
+template <typename Y, int BM, bool EX>
 __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     constexpr int IO = 8;                  // 16-output fragments of a wave
     constexpr int IT = BM / 32;            // 16-row fragments of a wave
@@ -442,7 +668,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     const int l16 = lane & 15, q = lane >> 4;
     const uint32_t rb = static_cast<uint32_t>(a.d_in) / 2;       // bytes of a code row
     const uint32_t sb = static_cast<uint32_t>(a.d_in) / 32;      // bytes of a scale row
-    const int np = a.d_in / kTlPair;       // even
+    const int np = (a.d_in + 2 * kTlPair - 1) / (2 * kTlPair) * 2;      // even
 
     // Tiles are numbered so that each XCD (workgroups are dealt to the 8 of
     // them in turn) walks one contiguous range, kTlGroupM row panels at a
@@ -483,17 +709,21 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     const uint32_t unit = 16u * static_cast<uint32_t>((lane & 7) ^ ((lane >> 4) | ((wave & 1) << 2)));
     const uint8_t *base_w, *base_x, *base_sw, *base_sx;
     uint32_t off_w[LW], off_x[LX], off_sw, off_sx;
+    // general rows: base_sw and base_sx are dword-aligned, and these the last
+    // offsets from them where 16 bytes may be read
+    uint32_t most_sw = 0, most_sx = 0;
     auto set_rows = [&]() {
         const int64_t w0 = static_cast<int64_t>(lt.group) * a.d_out + lt.n0;
         base_w = a.cw + w0 * rb;
         base_sw = a.ew + w0 * sb;
         const int left_w = a.d_out - lt.n0 < kTlN ? a.d_out - lt.n0 : kTlN;
         const int left_x = lt.end - lt.first < BM ? lt.end - lt.first : BM;
+        const uint32_t in_row = EX ? unit : 0u;
         // rows past the end read the last one (their results are not stored)
 #pragma unroll
         for (int j = 0; j < LW; ++j) {
             const int r = 8 * (4 * j + wave) + (lane >> 3);
-            off_w[j] = static_cast<uint32_t>(r < left_w ? r : left_w - 1) * rb + unit;
+            off_w[j] = static_cast<uint32_t>(r < left_w ? r : left_w - 1) * rb + in_row;
         }
         const int rw = 64 * wave + lane;
         off_sw = static_cast<uint32_t>(rw < left_w ? rw : left_w - 1) * sb;
@@ -505,8 +735,19 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
             return static_cast<uint32_t>(by_id ? mx4_source_row(a, lt.first + c) : c);
         };
 #pragma unroll
-        for (int j = 0; j < LX; ++j) off_x[j] = src(8 * (4 * j + wave) + (lane >> 3)) * rb + unit;
+        for (int j = 0; j < LX; ++j) off_x[j] = src(8 * (4 * j + wave) + (lane >> 3)) * rb + in_row;
         off_sx = src(64 * wave + lane) * sb;
+        if (!EX) {
+            auto align = [&](const uint8_t*& base, uint32_t& off, const uint8_t* first, int64_t rows) {
+                const uint32_t low = static_cast<uint32_t>(reinterpret_cast<uint64_t>(base)) & 3u;
+                base -= low;
+                off += low;
+                const int64_t at = ((rows * sb - 1) & ~int64_t{3}) - 12 - (base - first);
+                return static_cast<uint32_t>(at < (int64_t{1} << 31) ? at : (int64_t{1} << 31));
+            };
+            most_sw = align(base_sw, off_sw, a.ew, static_cast<int64_t>(a.groups) * a.d_out);
+            most_sx = align(base_sx, off_sx, a.ex, a.n);
+        }
     };
     set_rows();
     const uint32_t lds_codes =
@@ -517,15 +758,41 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         static_cast<uint32_t>(wave) * 1024u;
     auto load_codes = [&](int j, int buf) {            // j < NL
         const uint32_t dst = lds_codes + static_cast<uint32_t>(buf) * (ROWS * kTlUnits * 16u);
-        if (j < LW) mx4_copy16(base_w + ls * 128, off_w[j], dst + static_cast<uint32_t>(j) * 4096u);
-        else mx4_copy16(base_x + ls * 128, off_x[j - LW], dst + kTlN * 128u + static_cast<uint32_t>(j - LW) * 4096u);
+        const uint32_t col = static_cast<uint32_t>(ls) * 128u;
+        // general rows: past the end any unit of the row
+        const uint32_t at = EX ? 0u : (col + unit < rb ? col + unit : 0u);
+        if (j < LW) mx4_copy16(base_w + (EX ? col : 0u), off_w[j] + at, dst + static_cast<uint32_t>(j) * 4096u);
+        else mx4_copy16(base_x + (EX ? col : 0u), off_x[j - LW] + at, dst + kTlN * 128u + static_cast<uint32_t>(j - LW) * 4096u);
     };
     uint32_t load_super = 0;               // byte offset of the cursor's scale buffer
+    // General rows: the 16 bytes lie in the five dwords from the one that holds
+    // the first of them, the fifth copied to the wave's output space (which is
+    // not in use then).  At the buffer's end the 16 bytes begin earlier.
+    const uint32_t lds_fifth = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds_addr(&outs[wave][0])));
     auto load_scales = [&]() {             // before the codes of an even pair
-        const uint32_t dst = lds_scales + load_super;
-        mx4_copy16(base_sw + ls * 8, off_sw, dst);
-        if (BM == 256 || wave < BM / 64) mx4_copy16(base_sx + ls * 8, off_sx, dst + kTlN * 16u);
+        const uint32_t dst = lds_scales + load_super, col = static_cast<uint32_t>(ls) * 8u;
+        if (EX) {
+            mx4_copy16(base_sw + col, off_sw, dst);
+            if (BM == 256 || wave < BM / 64) mx4_copy16(base_sx + col, off_sx, dst + kTlN * 16u);
+        } else {
+            const uint32_t w = (off_sw & ~3u) + col, x = (off_sx & ~3u) + col;
+            mx4_copy16(base_sw, w < most_sw ? w : most_sw, dst);
+            mx4_copy4(base_sw, w + 4 < most_sw ? w + 16 : most_sw + 12, lds_fifth);
+            if (BM == 256 || wave < BM / 64) {
+                mx4_copy16(base_sx, x < most_sx ? x : most_sx, dst + kTlN * 16u);
+                mx4_copy4(base_sx, x + 4 < most_sx ? x + 16 : most_sx + 12, lds_fifth + 256u);
+            }
+        }
         load_super ^= ROWS * 16u;
+    };
+    // general rows: the token units past the end of pair `pair` in buffer `buf`
+    // count as zero
+    auto clear_tail = [&](int pair, int buf) {
+        if (EX || static_cast<uint32_t>(pair) * 128u + 128u <= rb) return;
+        if (static_cast<uint32_t>(pair) * 128u + unit < rb) return;
+#pragma unroll
+        for (int j = 0; j < LX; ++j)
+            codes[buf][kTlN * kTlUnits + (4 * j + wave) * kWave + lane] = u32x4{0u, 0u, 0u, 0u};
     };
 
     // ---- fragments
@@ -547,8 +814,25 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     // instruction only two wait states later, and the compiler does not see
     // the ones written as text.
     uint32_t turn_super = 0;
-    auto turn = [&](u32x4* p) {
-        const u32x4 v = *p;
+    auto turn = [&](u32x4* p, const uint32_t* fifth, uint32_t off, uint32_t most, int pair) {
+        u32x4 v = *p;
+        if (!EX) {
+            uint32_t w[5] = {v[0], v[1], v[2], v[3], *fifth};
+            const uint32_t at = (off & ~3u) + static_cast<uint32_t>(pair) * 8u;
+            const uint32_t early = at > most ? (at - most) / 4u : 0u;      // dwords
+#pragma unroll
+            for (uint32_t t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = early > t ? w[i + 1] : w[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = __builtin_amdgcn_alignbyte(w[i + 1], w[i], off & 3u);
+                // blocks past the row's end: scale 1
+                const int left = static_cast<int>(sb) - pair * 8 - 4 * i;
+                const uint32_t keep = left >= 4 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+                v[i] = (v[i] & keep) | (0x7F7F7F7Fu & ~keep);
+            }
+        }
         const uint32_t a0 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u);    // 00 10 01 11
         const uint32_t a1 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602u);    // 02 12 03 13
         const uint32_t b0 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u);
@@ -556,10 +840,11 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         *p = u32x4{__builtin_amdgcn_perm(b0, a0, 0x05040100u), __builtin_amdgcn_perm(b0, a0, 0x07060302u),
                    __builtin_amdgcn_perm(b1, a1, 0x05040100u), __builtin_amdgcn_perm(b1, a1, 0x07060302u)};
     };
-    auto turn_scales = [&]() {
+    auto turn_scales = [&](int pair) {     // of this pair and the next
         u32x4* const p = &scales[0][turn_super + 64 * wave + lane];
-        turn(p);
-        if (BM == 256 || wave < BM / 64) turn(p + kTlN);
+        const uint32_t* const fifth = reinterpret_cast<const uint32_t*>(&outs[wave][0]) + lane;
+        turn(p, fifth, off_sw, most_sw, pair);
+        if (BM == 256 || wave < BM / 64) turn(p + kTlN, fifth + kWave, off_sx, most_sx, pair);
         turn_super ^= ROWS;
     };
     const int* const rd_sw = reinterpret_cast<const int*>(&scales[0][wo * 128 + l16]) + q;
@@ -639,7 +924,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     // are read.  Copy c of a pair is issued SP c steps behind the barrier of a
     // second stage, the last ones in the stage after it.
     constexpr int BAR = (IT - 3) * IO - 1, AFTER = NM - 1 - BAR, SP = IT / 2;
-    constexpr int BEGUN = AFTER / SP + 1;  // copies issued before that stage ends
+    constexpr int BEGUN = AFTER / SP + 1 < NL ? AFTER / SP + 1 : NL;   // copies issued before that stage ends
     static_assert((NL - 1) * SP < AFTER + BAR, "copies are issued before the scales are waited for");
 
     // ---- prologue: pair 0 and the begun part of pair 1 (np >= 2)
@@ -651,7 +936,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     for (int j = 0; j < BEGUN; ++j) load_codes(j, 1);
     wait_vmcnt<BEGUN>();
     asm volatile("" ::: "memory");
-    turn_scales();
+    turn_scales(0);
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < IO; ++i) {
@@ -677,12 +962,13 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
             if (m == BAR) {
                 if (B % 2 == 1) {
                     wait_vmcnt<0>();
+                    if (!EX) clear_tail(ls > 0 ? ls - 1 : np - 1, B == 1 ? 1 : 0);
                     lds_barrier();
                     if (B == 1) load_scales();
                 } else if (B == 2) {
                     wait_vmcnt<NL>();
                     asm volatile("" ::: "memory");
-                    turn_scales();
+                    turn_scales(ls);
                 }
                 if (B == 3) {
                     read_super ^= 4 * ROWS;
@@ -726,61 +1012,141 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     wait_vmcnt<0>();                       // the requests past the last pair
 }
 
-// Large tiles need whole pairs of stages (scale rows of whole 16 bytes) and
-// 32-bit offsets into gathered rows.
-static bool tile_fits(const Mx4Args& a) {
-    return a.d_in % 512 == 0 &&
-           (!a.row_ids || static_cast<int64_t>(a.n) * (a.d_in / 2) < (int64_t{1} << 32));
-}
-
-template <int BM>
-static hipError_t launch_tiles(const Mx4Args& a, int y_bf16, hipStream_t stream) {
-    int dev = 0, cus = 0;
-    hipError_t err = hipGetDevice(&dev);
-    if (err == hipSuccess) err = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
-    if (err != hipSuccess) return err;
-    const unsigned grid = static_cast<unsigned>(cus >= kMxXcd ? cus / kMxXcd * kMxXcd : kMxXcd);
-    if (y_bf16) mx4_tile_kernel<uint16_t, BM><<<grid, kTlThreads, 0, stream>>>(a);
-    else mx4_tile_kernel<float, BM><<<grid, kTlThreads, 0, stream>>>(a);
-    return hipGetLastError();
-}
-
+// ---------------------------------------------------------------- dispatch
 // Tile shapes of the split kernel: rows / 16, outputs / 16, ring chunks.
-struct SpTile {
-    int a, b;
+#define CAT_SPLIT_TILES(V) V(0, 1, 1, 4) V(1, 1, 2, 4) V(2, 1, 4, 3) V(3, 2, 4, 2) V(4, 4, 4, 2)
+// Of the line kernel: rows / 16, outputs / 16, ring chunks, waves.
+#define CAT_LINE_TILES(V) \
+    V(0, 1, 1, 2, 8) V(1, 1, 2, 2, 4) V(2, 1, 4, 1, 4) V(3, 2, 2, 2, 4) V(4, 2, 4, 1, 4) V(5, 3, 4, 1, 4) \
+    V(6, 4, 4, 1, 4)
+struct SmallTile {
+    int a, b, d, w;
 };
-#define CAT_SPLIT_TILES(V) \
-    V(0, 1, 1, 4) V(1, 1, 2, 4) V(2, 1, 4, 3) V(3, 2, 2, 4) V(4, 2, 4, 2) V(5, 3, 4, 2) V(6, 5, 4, 2) V(7, 4, 4, 2)
-#define CAT_SPLIT_AB(id, A, B, D) {A, B},
-static constexpr SpTile kSpTiles[] = {CAT_SPLIT_TILES(CAT_SPLIT_AB)};
-#undef CAT_SPLIT_AB
+#define CAT_SHAPE(id, A, B, D) {A, B, D, kSpWaves},
+static constexpr SmallTile kSpTiles[] = {CAT_SPLIT_TILES(CAT_SHAPE)};
+#undef CAT_SHAPE
+#define CAT_SHAPE(id, A, B, D, W) {A, B, D, W},
+static constexpr SmallTile kLnTiles[] = {CAT_LINE_TILES(CAT_SHAPE)};
+#undef CAT_SHAPE
+
 // A launch covers fewer than 2^32 threads; workgroups then take several tiles.
 constexpr int64_t kSpMaxGrid = int64_t{1} << 22;
-constexpr int kSpTileCount = sizeof(kSpTiles) / sizeof(kSpTiles[0]);
+static unsigned small_grid(const Mx4Args& a, int bm, int bn) {
+    const int64_t T = mx4_row_tiles_most(a, bm) * ((a.d_out + bn - 1) / bn);
+    const int64_t wgs = (T + kMxXcd - 1) / kMxXcd * kMxXcd;
+    return static_cast<unsigned>(wgs < kSpMaxGrid ? wgs : kSpMaxGrid);
+}
 
 template <typename Y, bool ALN>
 static hipError_t launch_split(const Mx4Args& a, int tile, hipStream_t stream) {
-    const SpTile& t = kSpTiles[tile];
-    const int64_t T = mx4_row_tiles_most(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
-    const int64_t wgs = (T + kMxXcd - 1) / kMxXcd * kMxXcd;
-    const dim3 grid(static_cast<unsigned>(wgs < kSpMaxGrid ? wgs : kSpMaxGrid));
     switch (tile) {
-#define CAT_SPLIT_CASE(id, A, B, D) \
-    case id: mx4_split_kernel<Y, A, B, sp_depth(A, B, D, ALN), ALN><<<grid, kSpThreads, 0, stream>>>(a); break;
-        CAT_SPLIT_TILES(CAT_SPLIT_CASE)
-#undef CAT_SPLIT_CASE
+#define CAT_CASE(id, A, B, D)                                                             \
+    case id:                                                                              \
+        mx4_split_kernel<Y, A, B, D, ALN>                                                 \
+            <<<small_grid(a, 16 * A, 16 * B), kSpThreads, 0, stream>>>(a);                \
+        break;
+        CAT_SPLIT_TILES(CAT_CASE)
+#undef CAT_CASE
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
 }
 
-static hipError_t launch(const Mx4Args& a, int y_bf16, hipStream_t stream) {
-    int tile = a.m > 64 ? 7 : a.m > 32 ? 5 : a.m > 16 ? 3 : 0;
-    if (a.m >= 256 && tile_fits(a)) tile = kSpTileCount;
-    if (tile == kSpTileCount) return launch_tiles<256>(a, y_bf16, stream);
-    if (a.d_in % 128 == 0)
-        return y_bf16 ? launch_split<uint16_t, true>(a, tile, stream) : launch_split<float, true>(a, tile, stream);
-    return y_bf16 ? launch_split<uint16_t, false>(a, tile, stream) : launch_split<float, false>(a, tile, stream);
+template <typename Y, bool EX>
+static hipError_t launch_line(const Mx4Args& a, int tile, hipStream_t stream) {
+    switch (tile) {
+#define CAT_CASE(id, A, B, D, W)                                                          \
+    case id:                                                                              \
+        mx4_line_kernel<Y, A, B, D, W, EX>                                                \
+            <<<small_grid(a, 16 * A, 16 * B), W * kWave, 0, stream>>>(a);                 \
+        break;
+        CAT_LINE_TILES(CAT_CASE)
+#undef CAT_CASE
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+template <typename Y, int BM, bool EX>
+static hipError_t launch_tiles(const Mx4Args& a, int cus, hipStream_t stream) {
+    const unsigned grid = static_cast<unsigned>(cus >= kMxXcd ? cus / kMxXcd * kMxXcd : kMxXcd);
+    mx4_tile_kernel<Y, BM, EX><<<grid, kTlThreads, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+// Row tiles to expect.  Where rows go is known on the device only: taken as
+// spread evenly over the experts, each of which ends inside a tile.
+static double row_tiles(const Mx4Args& a, int bm) {
+    if (!a.offsets) return static_cast<double>((a.m + bm - 1) / bm);
+    const double used = a.groups * (1.0 - std::exp(-static_cast<double>(a.m) / a.groups));
+    const double full = static_cast<double>(a.m) / bm + 0.5 * used;
+    return used > full ? used : full;
+}
+
+// Estimated nanoseconds.  Small tiles: the workgroups of a CU that fit its LDS
+// and waves run together, so a CU's tiles cost their rounds at the latency of
+// the chunks of a wave (950 ns each, 570 with two in flight) or their sum at
+// the rate of its copies (14.4 ns each) and of the sums, whichever is longer.
+// Large tiles: rounds of one tile a CU, pairs and a fixed part.  Over 550
+// random shapes (1 to 4096 rows, dense and by up to 128 experts, 1024 to
+// 14336 inputs, 128 to 16384 outputs) the shape with the least estimate took
+// 2.4% longer than the fastest of the nine.
+static double line_cost(const Mx4Args& a, const SmallTile& t, int cus) {
+    const int l = t.a + t.b, copies = 2 * l + (l + 3) / 4, pieces = (a.d_in + 255) / 256;
+    const int wave_bytes = ln_wave_bytes(t.a, t.b, t.d, t.w);
+    const int by_lds = 160 * 1024 / (wave_bytes * t.w), by_waves = (l > 5 ? 16 : 24) / t.w;
+    const int together = by_lds < by_waves ? by_lds : by_waves;
+    const double tiles = row_tiles(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
+    const double per_cu = std::ceil(tiles / cus), rounds = std::ceil(per_cu / together);
+    const double latency = 1000.0 + (t.d == 2 ? 570.0 : 950.0) * ((pieces + t.w - 1) / t.w) + 6.0 * copies;
+    const double work = 14.4 * pieces * copies + 70.0 * t.a * t.b + 500.0;
+    const double by_work = per_cu * work + 700.0;
+    return 2000.0 + (rounds * latency > by_work ? rounds * latency : by_work);
+}
+static double tile_cost(const Mx4Args& a, int bm, int cus) {
+    const int pairs = (a.d_in + 511) / 512 * 2;
+    const double tiles = row_tiles(a, bm) * ((a.d_out + kTlN - 1) / kTlN), rounds = std::ceil(tiles / cus);
+    return bm == 128 ? rounds * (800.0 * pairs + 8700.0) - 2400.0 : rounds * (1200.0 * pairs + 11400.0) - 3400.0;
+}
+// Short rows (the split kernel): all its waves together hold the whole
+// reduction, so a tile is a fixed part, its copies and its sums.  2.7% over
+// the fastest of the five at 200 random shapes.
+static double split_cost(const Mx4Args& a, const SmallTile& t, int cus) {
+    const int l = t.a + t.b, copies = l + (l + 3) / 4 * (a.d_in % 128 == 0 ? 1 : 2);
+    const double tiles = row_tiles(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
+    return std::ceil(tiles / cus) * (10.0 * ((a.d_in + 127) / 128) * copies + 50.0 * t.a * t.b + 1200.0);
+}
+
+template <typename Y>
+static hipError_t launch(const Mx4Args& a, hipStream_t stream) {
+    int dev = 0, cus = 0;
+    hipError_t err = hipGetDevice(&dev);
+    if (err == hipSuccess) err = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+    if (err != hipSuccess) return err;
+    int pick = 0;
+    double best = 0.0;
+    auto offer = [&](int id, double cost) {
+        if (id == 0 || cost < best) {
+            best = cost;
+            pick = id;
+        }
+    };
+    if (a.d_in < 512) {
+        constexpr int n = sizeof(kSpTiles) / sizeof(kSpTiles[0]);
+        for (int i = 0; i < n; ++i) offer(i, split_cost(a, kSpTiles[i], cus));
+        return a.d_in % 128 == 0 ? launch_split<Y, true>(a, pick, stream) : launch_split<Y, false>(a, pick, stream);
+    }
+    constexpr int n = sizeof(kLnTiles) / sizeof(kLnTiles[0]);
+    for (int i = 0; i < n; ++i) offer(i, line_cost(a, kLnTiles[i], cus));
+    // the large tiles take 32-bit offsets into gathered rows
+    if (!a.row_ids || static_cast<int64_t>(a.n) * (a.d_in / 2) < (int64_t{1} << 32)) {
+        offer(n, tile_cost(a, 128, cus));
+        offer(n + 1, tile_cost(a, 256, cus));
+    }
+    const bool ex = a.d_in % 512 == 0;
+    if (pick == n) return ex ? launch_tiles<Y, 128, true>(a, cus, stream) : launch_tiles<Y, 128, false>(a, cus, stream);
+    if (pick == n + 1) return ex ? launch_tiles<Y, 256, true>(a, cus, stream) : launch_tiles<Y, 256, false>(a, cus, stream);
+    return ex ? launch_line<Y, true>(a, pick, stream) : launch_line<Y, false>(a, pick, stream);
 }
 
 hipError_t launch_mx4_linear(const uint8_t* cx, const uint8_t* ex, const uint8_t* cw,
@@ -788,7 +1154,7 @@ hipError_t launch_mx4_linear(const uint8_t* cx, const uint8_t* ex, const uint8_t
                              int y_bf16, hipStream_t stream) {
     const Mx4Args a{cx, ex, cw, ew, nullptr, nullptr, y, static_cast<int>(n), static_cast<int>(n), 1,
                     static_cast<int>(d_in), static_cast<int>(d_out)};
-    return launch(a, y_bf16, stream);
+    return y_bf16 ? launch<uint16_t>(a, stream) : launch<float>(a, stream);
 }
 
 hipError_t launch_mx4_linear_grouped(const uint8_t* cx, const uint8_t* ex, int64_t n,
@@ -798,7 +1164,7 @@ hipError_t launch_mx4_linear_grouped(const uint8_t* cx, const uint8_t* ex, int64
                                      hipStream_t stream) {
     const Mx4Args a{cx, ex, cw, ew, row_ids, offsets, y, static_cast<int>(n), static_cast<int>(m),
                     static_cast<int>(groups), static_cast<int>(d_in), static_cast<int>(d_out)};
-    return launch(a, y_bf16, stream);
+    return y_bf16 ? launch<uint16_t>(a, stream) : launch<float>(a, stream);
 }
 
 }  // namespace catk
