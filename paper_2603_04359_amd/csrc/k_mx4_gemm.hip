@@ -866,20 +866,32 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     // (16-byte unit u of row r at u ^ r), so that 16 lanes store 256
     // contiguous bytes of a row: stored from the accumulators, pieces of 32
     // bytes, a prefill's y took 68 us of 289.
-    auto sum = [&](int i, int j, int e) {
-        // read in place: as an ordinary value all 256 would change registers
-        float v;
-        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[i][j][e]));
-        return v;
-    };
     u32x4* const out_lds = &outs[wave][0];
-    auto store = [&](const Tile& t) {
-        // the last matrix step's result takes up to 18 wait states
-        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    // FULL: all of the wave's outputs exist; VEC: 16-byte stores at 32-bit
+    // offsets from the wave's first output.
+    auto store_as = [&](const Tile& t, auto full_, auto vec_) {
+        constexpr bool FULL = decltype(full_)::value, VEC = decltype(vec_)::value;
+        // what depends on the lane is computed here again: kept through the
+        // stages it would take their registers
+        int el = lane;
+        asm volatile("" : "+v"(el));
+        const int l16 = el & 15, q = el >> 4;
+        // The last matrix step's result takes up to 18 wait states; the reads
+        // below come behind them because they take `ready`.  They read in
+        // place: as ordinary values all 256 sums would change registers.
+        int ready;
+        asm volatile("s_nop 15\n\ts_nop 15\n\ts_mov_b32 %0, 0" : "=s"(ready)::"memory");
+        auto sum = [&](int i, int j, int e) {
+            float v;
+            asm("v_accvgpr_read_b32 %0, %1 ; %2" : "=v"(v) : "a"(acc[i][j][e]), "s"(ready));
+            return v;
+        };
         constexpr int PER = 16 / sizeof(Y);            // outputs of a unit
         constexpr int PARTS = sizeof(Y) == 4 ? 2 : 1;  // 256-byte pieces of a wave's row
-        const int rows = t.end - t.first, cols = a.d_out - t.n0;
-        const bool vec = a.d_out % PER == 0;
+        const int rows = t.end - t.first - wt * (BM / 2), cols = a.d_out - t.n0 - wo * 128;
+        Y* const yw = static_cast<Y*>(a.y) + static_cast<int64_t>(t.first + wt * (BM / 2)) * a.d_out + t.n0 + wo * 128;
+        const uint32_t pitch = static_cast<uint32_t>(a.d_out) * sizeof(Y);
+        const uint32_t at = static_cast<uint32_t>(q) * pitch + static_cast<uint32_t>(l16) * 16u;
 #pragma unroll
         for (int j = 0; j < IT; ++j) {
 #pragma unroll
@@ -896,27 +908,37 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
                             u32x2{pack_bf16(v0, v1), pack_bf16(v2, v3)};
                     }
                 }
+                u32x4 v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = out_lds[(4 * r + q) * 16 + (l16 ^ (4 * r + q))];
+                const int c = h * (128 / PARTS) + l16 * PER;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int lr = 4 * r + q;          // 16 lanes a row
-                    const u32x4 v = out_lds[lr * 16 + (l16 ^ lr)];
-                    const int row = wt * (BM / 2) + 16 * j + lr;
-                    const int c = wo * 128 + h * (128 / PARTS) + l16 * PER;
-                    if (row >= rows || c >= cols) continue;
-                    Y* y = static_cast<Y*>(a.y) + static_cast<int64_t>(t.first + row) * a.d_out + t.n0 + c;
-                    if (vec) {
-                        *reinterpret_cast<u32x4*>(y) = v;
+                    const int row = 16 * j + 4 * r + q;            // 16 lanes a row
+                    if (!FULL && (row >= rows || c >= cols)) continue;
+                    if constexpr (VEC) {
+                        char* const base = reinterpret_cast<char*>(yw + h * (128 / PARTS)) + static_cast<uint64_t>(16 * j + 4 * r) * pitch;
+                        *reinterpret_cast<u32x4*>(base + at) = v[r];
                     } else {
+                        Y* const y = yw + static_cast<int64_t>(row) * a.d_out + c;
 #pragma unroll
                         for (int e = 0; e < PER; ++e) {
                             if (c + e >= cols) continue;
-                            if constexpr (sizeof(Y) == 4) y[e] = __uint_as_float(v[e]);
-                            else y[e] = static_cast<uint16_t>(v[e / 2] >> (16 * (e % 2)));
+                            if constexpr (sizeof(Y) == 4) y[e] = __uint_as_float(v[r][e]);
+                            else y[e] = static_cast<uint16_t>(v[r][e / 2] >> (16 * (e % 2)));
                         }
                     }
                 }
             }
         }
+    };
+
+    auto store = [&](const Tile& t) {
+        const bool full = t.end - t.first - wt * (BM / 2) >= BM / 2 && a.d_out - t.n0 - wo * 128 >= 128;
+        const bool vec = a.d_out % (16 / sizeof(Y)) == 0 && a.d_out < (1 << 22);
+        if (full && vec) store_as(t, std::true_type{}, std::true_type{});
+        else if (vec) store_as(t, std::false_type{}, std::true_type{});
+        else store_as(t, std::false_type{}, std::false_type{});
     };
 
     // The barrier of a stage comes behind row IT - 4 of its matrix steps; the
@@ -1074,13 +1096,13 @@ static hipError_t launch_tiles(const Mx4Args& a, int cus, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Row tiles to expect.  Where rows go is known on the device only: taken as
-// spread evenly over the experts, each of which ends inside a tile.
+// Row tiles to expect.  Where rows go is known on the device only: their
+// counts are taken as exponentially distributed over the experts that have
+// any (a router prefers some), which gives 1 / (1 - exp(-bm / mean)) tiles each.
 static double row_tiles(const Mx4Args& a, int bm) {
     if (!a.offsets) return static_cast<double>((a.m + bm - 1) / bm);
     const double used = a.groups * (1.0 - std::exp(-static_cast<double>(a.m) / a.groups));
-    const double full = static_cast<double>(a.m) / bm + 0.5 * used;
-    return used > full ? used : full;
+    return used / (1.0 - std::exp(-bm * used / a.m));
 }
 
 // Estimated nanoseconds.  Small tiles: the workgroups of a CU that fit its LDS
