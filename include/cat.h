@@ -429,7 +429,8 @@ int cat_sqnr_terms(const float* s_x, int64_t n, int bits_x,
  *   one with a NaN or an infinity in h (or in fl(h * weight)) gets s_x = NaN
  *   and zero codes, so that its outputs are NaN.
  * cat_rmsnorm_mx4: MXFP4 codes and scales of y with the arithmetic of
- *   cat_mx4_quant: the operand of cat_mx4_linear.
+ *   cat_mx4_quant: the operand of cat_mx4_linear.  A token with a NaN or an
+ *   infinity in h gets the scale byte 255 (NaN) and zero codes throughout.
  *
  * x         device [n x d], x_dtype.  n >= 1; d >= 1, and d % 32 == 0 for
  *           cat_rmsnorm_mx4.
@@ -489,7 +490,8 @@ int cat_mx4_dequant(const uint8_t* codes, const uint8_t* scales, int64_t n,
  *   y[t, o] = sum_j x[t, j] * w[o, j]
  * of the values the codes stand for; products are exact, sums fp32 (in an
  * order that depends on the sizes only: repeated calls give identical
- * bits), y rounded once to y_dtype.
+ * bits), y rounded once to y_dtype.  Sums beyond fp32's range are infinite,
+ * or NaN where infinities of both signs meet; below it they round to 0.
  * codes_x  device uint8 [n x d_in/2], scales_x device uint8 [n x d_in/32].
  * codes_w  device uint8 [d_out x d_in/2], scales_w device uint8
  *          [d_out x d_in/32].

@@ -628,7 +628,9 @@ __device__ __forceinline__ int mx4_row_tiles(const Mx4Args& a) {
     }
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) tiles += __shfl_xor(tiles, o);
-    return tiles;
+    // offsets that decrease could give more: never more work than that
+    const int64_t most = mx4_row_tiles_most(a, BM);
+    return tiles < 0 || tiles > most ? static_cast<int>(most) : tiles;
 }
 
 // One matrix step with scale byte S of sw and sx, the sum in place in the

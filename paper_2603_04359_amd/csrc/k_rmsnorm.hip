@@ -62,9 +62,11 @@ __device__ __forceinline__ RowStats row_stats(RowStats s) {
     return s;
 }
 
+// NaN for a row that is not finite, so that all of it becomes NaN.
 __device__ __forceinline__ float inverse_rms(double ss, int64_t d, double eps) {
     const double v = ss / static_cast<double>(d) + eps;
-    return v > 0.0 ? static_cast<float>(1.0 / sqrt(v)) : (v == 0.0 ? 0.0f : __uint_as_float(0x7FC00000u));
+    if (v == 0.0) return 0.0f;
+    return v < __builtin_huge_val() ? static_cast<float>(1.0 / sqrt(v)) : __uint_as_float(0x7FC00000u);
 }
 
 // The int8 quantizer of a row: its scale, the factor of the codes, and a mask

@@ -328,12 +328,27 @@ def test_grouped_bad_offsets_and_ids_stay_in_bounds():
     cx, sx = _codes(m, d_in, 1)
     cw, sw = _codes(groups * d_out, d_in, 2)
     cw, sw = cw.reshape(groups, d_out, -1), sw.reshape(groups, d_out, -1)
-    for off in ([0, 5, 3, 50], [-7, 4, 30, 10], [2 ** 31 - 1] * 4, [20, 15, 10, 0]):
+    for off in ([0, 5, 3, 50], [-7, 4, 30, 10], [2 ** 31 - 1] * 4, [20, 15, 10, 0], [0, 20, 0, 20]):
         buf = torch.full((m + 64, d_out), 7.0, device="cuda")
         y = buf[32:32 + m]
         ids = _dev(np.array([-1, 2 ** 31 - 1, 0, 400] * 5, np.int32))
         _cat().cat_mx4_linear_grouped(_dev(cx), _dev(sx), _dev(np.array(off, np.int64).astype(np.int32)),
                                       _dev(cw), _dev(sw), y, row_ids=ids)
+        torch.cuda.synchronize()
+        assert (buf[:32] == 7).all() and (buf[32 + m:] == 7).all()
+
+
+def test_grouped_bad_offsets_on_large_tiles():
+    torch = torch_mod()
+    groups, d_in, d_out, m = 8, 512, 600, 4000
+    cx, sx = _codes(m, d_in, 1)
+    cw, sw = _codes(groups * d_out, d_in, 2)
+    cw, sw = _dev(cw.reshape(groups, d_out, -1)), _dev(sw.reshape(groups, d_out, -1))
+    cx, sx = _dev(cx), _dev(sx)
+    for off in ([0, 4000] * 4 + [0], [9, 5000, 3, -4, 4000, 10, 2 ** 31 - 1, 0, 77], [-2 ** 31] * 9):
+        buf = torch.full((m + 64, d_out), 7.0, device="cuda")
+        _cat().cat_mx4_linear_grouped(cx, sx, _dev(np.array(off, np.int64).astype(np.int32)), cw, sw,
+                                      buf[32:32 + m])
         torch.cuda.synchronize()
         assert (buf[:32] == 7).all() and (buf[32 + m:] == 7).all()
 

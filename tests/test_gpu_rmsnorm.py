@@ -142,13 +142,11 @@ def test_int8_non_finite_rows(d):
 
 @pytest.mark.parametrize("d", [64, 4096, 33024])
 def test_mx4_non_finite_rows(d):
-    # the whole row's norm is not finite: NaN blocks, or zeros beside an
-    # infinity (h / inf); other rows are untouched
+    # the whole row's norm is not finite; other rows are untouched
     x = _rows(4, d, 1)
     x[1, 3], x[2, d - 1] = np.nan, np.inf
     (_, w, _), c, s, _ = _run(4, d, "bf16", "bf16", False, True, x=x)
-    assert (s[1] == 255).all() and (c[1] == 0).all()
-    assert s[2, -1] == 255
+    assert (s[1:3] == 255).all() and (c[1:3] == 0).all()
     ok = [0, 3]
     co, so = mo.quantize(mo.rmsnorm_f32(mo.round_bf16(x[ok]), w, eps=1e-5)[1])
     assert np.array_equal(s[ok], so) and np.array_equal(c[ok], co)
