@@ -2,7 +2,24 @@
 //   y[i, o] = sum_b 2^(ex[i, b] + ew[o, b] - 254) sum_{j in b} cx[i, j] cw[o, j]
 // on the block-scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4:
 // lane L holds row L % 16, elements [32 (L / 16), 32 (L / 16) + 32) of a
-// step of 128 (16 bytes of codes) and that block's scale byte.
+// step of 128 (16 bytes of codes) and that block's scale byte.  Weights are
+// the first operand, so that a lane's four sums are consecutive outputs.
+//
+// The order of the reduction is free as long as both operands take the same,
+// which every kernel here uses to load whole pieces of rows.
+//
+// Three forms, picked by an estimate of their times (at the end):
+//   line   few rows: small tiles, their reduction shared out among the waves of
+//          a workgroup; bound by the weights' bytes
+//   tile   many rows: 128 x 256 or 256 x 256 outputs a workgroup; bound by the
+//          matrix rate, which the power of random data holds at 6.6 to 7
+//          PFLOP/s of the nominal 10
+//   split  rows of less than 512 elements
+// Kernel times, weights in the last-level cache (rows x inputs -> outputs):
+//   1 x 4096 -> 4096 3.4 us, 48 x 4096 -> 14336 8.6 us, 100 x 4096 -> 4096
+//   6.5 us, 257 x 14336 -> 4096 29 us, 1000 x 4096 -> 4096 20 us, 8192 x 4096
+//   -> 14336 228 to 245 us (3.9 to 4.2 PFLOP/s); 128 rows of 64 experts 2048
+//   -> 1024 10 us, 16384 rows of 8 uneven experts 14336 -> 4096 520 us (3.7).
 #include <cmath>
 #include <type_traits>
 
@@ -170,15 +187,51 @@ __device__ __forceinline__ void mx4_copy4(const uint8_t* p, uint32_t lds) {
 constexpr int kSpWaves = 8;
 constexpr int kSpThreads = kSpWaves * kWave;
 
-// LDS of a wave: its ring, later its partial sums of a round of at most 8
-// accumulators.
+// Accumulators whose partial sums are added at a time: one per wave.
+constexpr int mx4_round(int a, int b, int w) { return a * b < w ? a * b : w; }
+// LDS of a wave: its ring, later its partial sums of a round.
+constexpr int mx4_wave_bytes(int a, int b, int w, int ring) {
+    return ring > mx4_round(a, b, w) * 1024 ? ring : mx4_round(a, b, w) * 1024;
+}
 constexpr int sp_stage_bytes(int a, int b, bool aligned) {
     return (a + b) * 1024 + (a + b + 3) / 4 * 256 * (aligned ? 1 : 2);
 }
-constexpr int sp_round(int a, int b) { return a * b < 8 ? a * b : 8; }
 constexpr int sp_wave_bytes(int a, int b, int d, bool aligned) {
-    return d * sp_stage_bytes(a, b, aligned) > sp_round(a, b) * 1024 ? d * sp_stage_bytes(a, b, aligned)
-                                                                     : sp_round(a, b) * 1024;
+    return mx4_wave_bytes(a, b, kSpWaves, d * sp_stage_bytes(a, b, aligned));
+}
+
+// Adds the W waves' partial sums of a tile, in the waves' order, through LDS
+// and stores them.
+template <typename Y, int A, int B, int W, int BYTES>
+__device__ __forceinline__ void mx4_join(const Mx4Args& a, const Mx4Rows& r, int n0,
+                                         uint8_t (&lds)[W][BYTES], const f32x4 (&acc)[A][B]) {
+    constexpr int RT = mx4_round(A, B, W), ROUNDS = (A * B + RT - 1) / RT;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int rows_x = r.end - r.first, rows_w = a.d_out - n0;
+#pragma unroll
+    for (int rd = 0; rd < ROUNDS; ++rd) {
+        __syncthreads();                   // the ring (or the last round) is read
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int tl = rd * RT + t;
+            if (tl < A * B) reinterpret_cast<f32x4*>(&lds[wave][0])[t * kWave + lane] = acc[tl / B][tl % B];
+        }
+        __syncthreads();
+        const int tl = rd * RT + wave;
+        if (wave < RT && tl < A * B) {
+            f32x4 v = reinterpret_cast<const f32x4*>(&lds[0][0])[wave * kWave + lane];
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                const f32x4 p = reinterpret_cast<const f32x4*>(&lds[w][0])[wave * kWave + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += p[e];
+            }
+            // a lane holds row lane % 16, outputs 4 (lane / 16) .. + 3
+            mx4_store4(static_cast<Y*>(a.y), a.d_out, r.first, n0, rows_x, rows_w,
+                       (tl / B) * 16 + (lane & 15), (tl % B) * 16 + 4 * (lane >> 4), v);
+        }
+    }
 }
 
 template <typename Y, int A, int B, int D, bool ALN>
@@ -191,7 +244,6 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
     static_assert(COPIES * (D - 1) < 64, "copies in flight must fit the vmcnt range");
     constexpr int kScaleAt = L * 1024;     // bytes in a ring stage
     constexpr int kStageBytes = sp_stage_bytes(A, B, ALN);
-    constexpr int RT = sp_round(A, B);     // accumulators added per round
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int l16 = lane & 15, q = lane >> 4;
@@ -316,31 +368,7 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
         st = st + 1 == D ? 0 : st + 1;
     }
 
-    // partial sums, RT accumulators a round: lane holds row l16, outputs 4 q .. + 3
-    constexpr int ROUNDS = (A * B + RT - 1) / RT;
-#pragma unroll
-    for (int rd = 0; rd < ROUNDS; ++rd) {
-        __syncthreads();                   // the ring (or the last round) is read
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const int tl = rd * RT + t;
-            if (tl < A * B)
-                reinterpret_cast<f32x4*>(&lds[wave][0])[t * kWave + lane] = acc[tl / B][tl % B];
-        }
-        __syncthreads();
-        const int tl = rd * RT + wave;
-        if (wave < RT && tl < A * B) {
-            f32x4 v = reinterpret_cast<const f32x4*>(&lds[0][0])[wave * kWave + lane];
-#pragma unroll
-            for (int w = 1; w < kSpWaves; ++w) {
-                const f32x4 p = reinterpret_cast<const f32x4*>(&lds[w][0])[wave * kWave + lane];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += p[e];
-            }
-            mx4_store4(static_cast<Y*>(a.y), a.d_out, r.first, n0, rows_x, rows_w, (tl / B) * 16 + l16,
-                       (tl % B) * 16 + 4 * q, v);
-        }
-    }
+    mx4_join<Y, A, B, kSpWaves>(a, r, n0, lds, acc);
 }
 
 // The same with whole cache lines, for rows of at least 512 elements: a chunk
@@ -355,10 +383,8 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
 // and a lane finds its bytes in it; units past a row's end count as zero with
 // scale 1.
 constexpr int ln_stage_bytes(int a, int b) { return (2 * (a + b) + (a + b + 3) / 4) * 1024; }
-constexpr int ln_round(int a, int b, int w) { return a * b < w ? a * b : w; }
 constexpr int ln_wave_bytes(int a, int b, int d, int w) {
-    return d * ln_stage_bytes(a, b) > ln_round(a, b, w) * 1024 ? d * ln_stage_bytes(a, b)
-                                                               : ln_round(a, b, w) * 1024;
+    return mx4_wave_bytes(a, b, w, d * ln_stage_bytes(a, b));
 }
 
 template <typename Y, int A, int B, int D, int W, bool EX>
@@ -370,7 +396,6 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
     constexpr int COPIES = 2 * L + SC;
     static_assert(COPIES * (D - 1) < 64, "copies in flight must fit the vmcnt range");
     constexpr int kScaleAt = 2 * L * 1024, kStageBytes = ln_stage_bytes(A, B);
-    constexpr int RT = ln_round(A, B, W);  // accumulators added per round
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int l16 = lane & 15, q = lane >> 4;
@@ -520,31 +545,7 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
         st = st + 1 == D ? 0 : st + 1;
     }
 
-    // partial sums, RT accumulators a round: lane holds row l16, outputs 4 q .. + 3
-    constexpr int ROUNDS = (A * B + RT - 1) / RT;
-#pragma unroll
-    for (int rd = 0; rd < ROUNDS; ++rd) {
-        __syncthreads();                   // the ring (or the last round) is read
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const int tl = rd * RT + t;
-            if (tl < A * B)
-                reinterpret_cast<f32x4*>(&lds[wave][0])[t * kWave + lane] = acc[tl / B][tl % B];
-        }
-        __syncthreads();
-        const int tl = rd * RT + wave;
-        if (wave < RT && tl < A * B) {
-            f32x4 v = reinterpret_cast<const f32x4*>(&lds[0][0])[wave * kWave + lane];
-#pragma unroll
-            for (int w = 1; w < W; ++w) {
-                const f32x4 p = reinterpret_cast<const f32x4*>(&lds[w][0])[wave * kWave + lane];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += p[e];
-            }
-            mx4_store4(static_cast<Y*>(a.y), a.d_out, r.first, n0, rows_x, rows_w, (tl / B) * 16 + l16,
-                       (tl % B) * 16 + 4 * q, v);
-        }
-    }
+    mx4_join<Y, A, B, W>(a, r, n0, lds, acc);
 }
 
 // Tiles of the call, walked so that XCD x (workgroups are dealt to the 8 of
@@ -636,8 +637,8 @@ __device__ __forceinline__ int mx4_row_tiles(const Mx4Args& a) {
 // One matrix step with scale byte S of sw and sx, the sum in place in the
 // accumulation registers.  Written as an instruction because a wave's sums
 // fill that half of the register file: left to the builtin, they are moved
-// back and forth between the halves.  The steps' sums are used again no
-// sooner than NM / 2 steps later, so they need no waits among each other.
+// back and forth between the halves.  A sum is used again no sooner than 32
+// steps later, so the steps need no waits among each other.
 template <int S>
 __device__ __forceinline__ void mx4_mfma_acc(u32x4 a, u32x4 b, f32x4& acc, int sw, int sx) {
     static_assert(S >= 0 && S < 4, "scale byte");
