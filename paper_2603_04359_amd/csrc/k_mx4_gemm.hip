@@ -124,9 +124,13 @@ __device__ __forceinline__ void mx4_store4(Y* y, int d_out, int first, int n0, i
                                            int row, int col, f32x4 v) {
     if (row >= rows || col >= cols) return;
     y += static_cast<int64_t>(first + row) * d_out + n0 + col;
-    if ((d_out & 3) == 0) {
-        if constexpr (sizeof(Y) == 4) *reinterpret_cast<f32x4*>(y) = v;
-        else *reinterpret_cast<u32x2*>(y) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    if (col + 4 <= cols) {                 // stores of 8 and 16 bytes may start at any byte here
+        if constexpr (sizeof(Y) == 4) {
+            __builtin_memcpy(y, &v, 16);
+        } else {
+            const u32x2 p = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            __builtin_memcpy(y, &p, 8);
+        }
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -870,10 +874,10 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     // contiguous bytes of a row: stored from the accumulators, pieces of 32
     // bytes, a prefill's y took 68 us of 289.
     u32x4* const out_lds = &outs[wave][0];
-    // FULL: all of the wave's outputs exist; VEC: 16-byte stores at 32-bit
-    // offsets from the wave's first output.
-    auto store_as = [&](const Tile& t, auto full_, auto vec_) {
-        constexpr bool FULL = decltype(full_)::value, VEC = decltype(vec_)::value;
+    // FULL: all of the wave's outputs exist, and rows are addressed by 32-bit
+    // offsets from its first one.
+    auto store_as = [&](const Tile& t, auto full_) {
+        constexpr bool FULL = decltype(full_)::value;
         // what depends on the lane is computed here again: kept through the
         // stages it would take their registers
         int el = lane;
@@ -918,30 +922,31 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = 16 * j + 4 * r + q;            // 16 lanes a row
-                    if (!FULL && (row >= rows || c >= cols)) continue;
-                    if constexpr (VEC) {
+                    // 16-byte stores may start at any byte here
+                    if constexpr (FULL) {
                         char* const base = reinterpret_cast<char*>(yw + h * (128 / PARTS)) + static_cast<uint64_t>(16 * j + 4 * r) * pitch;
-                        *reinterpret_cast<u32x4*>(base + at) = v[r];
-                    } else {
+                        __builtin_memcpy(base + at, &v[r], 16);
+                    } else if (row < rows && c < cols) {
                         Y* const y = yw + static_cast<int64_t>(row) * a.d_out + c;
+                        if (c + PER <= cols) {
+                            __builtin_memcpy(y, &v[r], 16);
+                        } else {
 #pragma unroll
-                        for (int e = 0; e < PER; ++e) {
-                            if (c + e >= cols) continue;
-                            if constexpr (sizeof(Y) == 4) y[e] = __uint_as_float(v[r][e]);
-                            else y[e] = static_cast<uint16_t>(v[r][e / 2] >> (16 * (e % 2)));
+                            for (int e = 0; e < PER; ++e) {
+                                if (c + e >= cols) continue;
+                                if constexpr (sizeof(Y) == 4) y[e] = __uint_as_float(v[r][e]);
+                                else y[e] = static_cast<uint16_t>(v[r][e / 2] >> (16 * (e % 2)));
+                            }
                         }
                     }
                 }
             }
         }
     };
-
     auto store = [&](const Tile& t) {
         const bool full = t.end - t.first - wt * (BM / 2) >= BM / 2 && a.d_out - t.n0 - wo * 128 >= 128;
-        const bool vec = a.d_out % (16 / sizeof(Y)) == 0 && a.d_out < (1 << 22);
-        if (full && vec) store_as(t, std::true_type{}, std::true_type{});
-        else if (vec) store_as(t, std::false_type{}, std::true_type{});
-        else store_as(t, std::false_type{}, std::false_type{});
+        if (full && a.d_out < (1 << 22)) store_as(t, std::true_type{});
+        else store_as(t, std::false_type{});
     };
 
     // The barrier of a stage comes behind row IT - 4 of its matrix steps; the
