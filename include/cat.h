@@ -425,7 +425,8 @@ int cat_sqnr_terms(const float* s_x, int64_t n, int bits_x,
  * cat_rmsnorm_quant: per-token int8 codes with the arithmetic of
  *   cat_transform_quant at 8 bits (amax = max |y|, s_x = fl(amax / 127),
  *   code = clamp(rint(fl(y * fl(127 / amax))), -127, 127)): the operand of
- *   cat_int8_linear.  A token with amax == 0 gets s_x = 0 and zero codes;
+ *   cat_int8_linear.  A token with amax < 127 * 2^-128 (about 3.7e-37: 0, or
+ *   so small that 127 / amax overflows) gets s_x = 0 and zero codes;
  *   one with a NaN or an infinity in h (or in fl(h * weight)) gets s_x = NaN
  *   and zero codes, so that its outputs are NaN.
  * cat_rmsnorm_mx4: MXFP4 codes and scales of y with the arithmetic of
@@ -439,7 +440,8 @@ int cat_sqnr_terms(const float* s_x, int64_t n, int bits_x,
  *           itself (no other overlap).
  * weight    device [d], w_dtype.
  * eps       >= 0, finite.  (Where the mean of squares and eps are both 0, y
- *           = 0.)
+ *           = 0; with eps = 0 and a root mean square below 2^-128, r is
+ *           infinite and the token counts as not finite.)
  * codes     device, written: int8 [n x d], or uint8 [n x d/2] (MXFP4).
  * s_x       device fp32 [n], scales  device uint8 [n x d/32]; written.
  * Pointers are 16-byte aligned.  No workspace.  The calls may be captured

@@ -70,17 +70,18 @@ __device__ __forceinline__ float inverse_rms(double ss, int64_t d, double eps) {
 }
 
 // The int8 quantizer of a row: its scale, the factor of the codes, and a mask
-// of them (0 where the codes are to be 0: an all-zero row, or one that is not
-// finite).
+// of them (0 where the codes are to be 0: a row of zeros, one so small that
+// the factor is infinite, or one that is not finite).
 struct Int8Scale {
     float s, inv;
     uint32_t keep;
 };
 __device__ __forceinline__ Int8Scale int8_scale(uint32_t amax_hw, float r) {
     const float amax = __uint_as_float(amax_hw) * r;
-    if (amax == 0.0f) return {0.0f, 0.0f, 0u};
     if (!(abs_bits(amax) < 0x7F800000u)) return {__uint_as_float(0x7FC00000u), 0.0f, 0u};
-    return {amax / 127.0f, 127.0f / amax, 0xFFFFFFFFu};
+    const float inv = 127.0f / amax;
+    if (abs_bits(inv) == 0x7F800000u) return {0.0f, 0.0f, 0u};
+    return {amax / 127.0f, inv, 0xFFFFFFFFu};
 }
 // Code of y, in the low byte: adding 1.5 * 2^23 rounds the product to the
 // nearest integer, ties to even, and leaves its two's complement in the low

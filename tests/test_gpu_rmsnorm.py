@@ -250,3 +250,21 @@ def test_layer_of_experts_as_used():
     assert np.array_equal(ca.cpu().numpy(), co2) and np.array_equal(sa.cpu().numpy(), so2)
     ref, absum = mo.linear_grouped(co2, so2, offsets, cd.cpu().numpy(), sd.cpu().numpy(), m)
     assert (np.abs(y.double().cpu().numpy() - ref) <= (f / 32 + 16) * 2.0 ** -23 * absum).all()
+
+
+@pytest.mark.parametrize("d", [32, 63, 4096, 33024])
+def test_int8_rows_below_the_quantizer_are_zero(d):
+    # 127 / amax overflows for amax below 127 * 2^-128 = 3.73e-37: such a
+    # token has a zero scale and zero codes; the next larger one is quantized
+    x = np.ones((4, d), np.float32)
+    x[:, 0] = -1
+    x[1] *= 0.5
+    x[2] = 0
+    w = np.zeros(d, np.float32)
+    w[:2] = np.float32(3e-37)                    # |y| 3e-37 (1 - 2^-24 or so)
+    (_, _, _), c, s, _ = _run(4, d, "f32", "f32", False, False, x=x, w=w, eps=0.0)
+    assert (c == 0).all() and (s == 0).all()
+    w[1] = np.float32(-4e-37)
+    (_, _, _), c, s, _ = _run(4, d, "f32", "f32", False, False, x=x, w=w, eps=0.0)
+    q, so = mo.quantize_int8(mo.rmsnorm_f32(x, w, eps=0.0)[1])
+    assert np.array_equal(c, q) and np.array_equal(s, so) and (c[[0, 1, 3], 1] == -127).all()
