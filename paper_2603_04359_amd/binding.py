@@ -186,12 +186,14 @@ def _torch():
 
 
 _dtype_sets = {}
+_dtype_codes = {}       # the ABI's number of a dtype, once _types has been called
 
 
 def _types(name):
     """The dtypes an operand may have, as one tuple kept per set."""
     if not _dtype_sets:
         torch = _torch()
+        _dtype_codes.update({torch.float32: CAT_F32, torch.bfloat16: CAT_BF16})
         _dtype_sets.update(u8=(torch.uint8,), i8=(torch.int8,), i32=(torch.int32,),
                            f32=(torch.float32,), float=(torch.bfloat16, torch.float32))
     return _dtype_sets[name]
@@ -538,9 +540,9 @@ def cat_full_hadamard_weights(W_prime, k: int):
     return out
 
 
-def _one_device(stream, first, *others):
-    """Every tensor on one device, and that device the current one: kernels
-    are launched there, on the current stream or on `stream`."""
+def _launch_stream(stream, first, *others):
+    """The handle of `stream`, or of the current stream.  Kernels are launched
+    on the current device, so every tensor has to be there, and `stream` too."""
     dev = first.get_device()
     for t in others:
         if t is not None and t.get_device() != dev:
@@ -548,13 +550,16 @@ def _one_device(stream, first, *others):
     current = _current_device() if _current_device is not None else _torch().cuda.current_device()
     if dev != current:
         raise ValueError(f"tensors on cuda:{dev}, but the current device is cuda:{current}")
-    if stream is not None and stream.device_index != dev:
+    if stream is None:
+        return _raw_stream(dev) if _raw_stream is not None else _stream_ptr(None)
+    if stream.device_index != dev:
         raise ValueError(f"tensors on cuda:{dev}, stream on cuda:{stream.device_index}")
+    return stream.cuda_stream
 
 
 def _rmsnorm_args(x, weight, codes, scales, residual, residual_out, stream):
-    """Checks shared by the RMS norm calls; (n, d, pointers of x, residual,
-    residual_out and weight)."""
+    """Checks shared by the RMS norm calls; (n, d, dtype codes of x and weight,
+    pointers of x, residual, residual_out and weight, the stream)."""
     floats = _types("float")
     px = _dev_ptr(x, "x", floats)
     pw = _dev_ptr(weight, "weight", floats)
@@ -562,15 +567,17 @@ def _rmsnorm_args(x, weight, codes, scales, residual, residual_out, stream):
         raise ValueError("x must be [n, d]")
     n, d = x.shape
     _numel(weight, d, "weight")
-    pr = _dev_ptr(residual, "residual", (x.dtype,), allow_none=True)
-    po = _dev_ptr(residual_out, "residual_out", (x.dtype,), allow_none=True)
-    if (pr is None) != (po is None):
-        raise ValueError("residual and residual_out go together")
-    if pr is not None:
-        _shape(residual, (n, d), "residual")
-        _shape(residual_out, (n, d), "residual_out")
-    _one_device(stream, x, weight, codes, scales, residual, residual_out)
-    return n, d, px, pr, po, pw
+    pr = po = None
+    if residual is not None or residual_out is not None:
+        own = (x.dtype,)
+        pr = _dev_ptr(residual, "residual", own, allow_none=True)
+        po = _dev_ptr(residual_out, "residual_out", own, allow_none=True)
+        if pr is None or po is None:
+            raise ValueError("residual and residual_out go together")
+        _shape(residual, x.shape, "residual")
+        _shape(residual_out, x.shape, "residual_out")
+    st = _launch_stream(stream, x, weight, codes, scales, residual, residual_out)
+    return n, d, _dtype_codes[x.dtype], _dtype_codes[weight.dtype], px, pr, po, pw, st
 
 
 def cat_rmsnorm_quant(x, weight, codes, s_x, residual=None, residual_out=None, eps: float = 1e-6,
@@ -580,63 +587,66 @@ def cat_rmsnorm_quant(x, weight, codes, s_x, residual=None, residual_out=None, e
     receives h in x's dtype.  x, residual [n, d] bf16 or fp32."""
     pc = _dev_ptr(codes, "codes", _types("i8"))
     ps = _dev_ptr(s_x, "s_x", _types("f32"))
-    n, d, px, pr, po, pw = _rmsnorm_args(x, weight, codes, s_x, residual, residual_out, stream)
+    n, d, tx, tw, px, pr, po, pw, st = _rmsnorm_args(x, weight, codes, s_x, residual, residual_out,
+                                                     stream)
     _shape(codes, (n, d), "codes")
     _numel(s_x, n, "s_x")
     _check("cat_rmsnorm_quant",
-           lib().cat_rmsnorm_quant(px, _dtype_code(x), n, d, pr, po, pw, _dtype_code(weight), eps,
-                                   pc, ps, _stream_ptr(stream)))
+           lib().cat_rmsnorm_quant(px, tx, n, d, pr, po, pw, tw, eps, pc, ps, st))
 
 
 def cat_rmsnorm_mx4(x, weight, codes, scales, residual=None, residual_out=None, eps: float = 1e-6,
                     stream=None):
     """cat_rmsnorm_quant with MXFP4 output: codes uint8 [n, d/2] and scales
     uint8 [n, d/32]."""
-    pc = _dev_ptr(codes, "codes", _types("u8"))
-    ps = _dev_ptr(scales, "scales", _types("u8"))
-    n, d, px, pr, po, pw = _rmsnorm_args(x, weight, codes, scales, residual, residual_out, stream)
-    _mx4_shapes(codes, scales, (n,), d)
+    u8 = _types("u8")
+    pc = _dev_ptr(codes, "codes", u8)
+    ps = _dev_ptr(scales, "scales", u8)
+    n, d, tx, tw, px, pr, po, pw, st = _rmsnorm_args(x, weight, codes, scales, residual,
+                                                     residual_out, stream)
+    _mx4_shapes(codes, scales, n, d)
     _check("cat_rmsnorm_mx4",
-           lib().cat_rmsnorm_mx4(px, _dtype_code(x), n, d, pr, po, pw, _dtype_code(weight), eps,
-                                 pc, ps, _stream_ptr(stream)))
+           lib().cat_rmsnorm_mx4(px, tx, n, d, pr, po, pw, tw, eps, pc, ps, st))
 
 
-def _mx4_shapes(codes, scales, lead, d, codes_name="codes", scales_name="scales"):
-    if d % 32 == 0 and codes.shape == (*lead, d >> 1) and scales.shape == (*lead, d >> 5):
-        return
+def _mx4_blocks(d):
     if d % 32:
         raise ValueError(f"rows of {d} elements are not whole blocks of 32")
-    _shape(codes, (*lead, d // 2), codes_name)
-    _shape(scales, (*lead, d // 32), scales_name)
+
+
+def _mx4_shapes(codes, scales, n, d):
+    _mx4_blocks(d)
+    _shape(codes, (n, d >> 1), "codes")
+    _shape(scales, (n, d >> 5), "scales")
 
 
 def cat_mx4_quant(X, codes, scales, stream=None):
     """MXFP4 codes uint8 [n, d/2] and scales uint8 [n, d/32] of X [n, d]
     (bf16 or fp32; activations or weights)."""
+    u8 = _types("u8")
     px = _dev_ptr(X, "X", _types("float"))
-    pc = _dev_ptr(codes, "codes", _types("u8"))
-    ps = _dev_ptr(scales, "scales", _types("u8"))
+    pc = _dev_ptr(codes, "codes", u8)
+    ps = _dev_ptr(scales, "scales", u8)
     if X.dim() != 2:
         raise ValueError("X must be [n, d]")
     n, d = X.shape
-    _mx4_shapes(codes, scales, (n,), d)
-    _one_device(stream, X, codes, scales)
-    _check("cat_mx4_quant",
-           lib().cat_mx4_quant(px, _dtype_code(X), n, d, pc, ps, _stream_ptr(stream)))
+    _mx4_shapes(codes, scales, n, d)
+    st = _launch_stream(stream, X, codes, scales)
+    _check("cat_mx4_quant", lib().cat_mx4_quant(px, _dtype_codes[X.dtype], n, d, pc, ps, st))
 
 
 def cat_mx4_dequant(codes, scales, out, stream=None):
     """out [n, d] (bf16 or fp32): the values of MXFP4 codes and scales."""
-    pc = _dev_ptr(codes, "codes", _types("u8"))
-    ps = _dev_ptr(scales, "scales", _types("u8"))
+    u8 = _types("u8")
+    pc = _dev_ptr(codes, "codes", u8)
+    ps = _dev_ptr(scales, "scales", u8)
     po = _dev_ptr(out, "out", _types("float"))
     if out.dim() != 2:
         raise ValueError("out must be [n, d]")
     n, d = out.shape
-    _mx4_shapes(codes, scales, (n,), d)
-    _one_device(stream, codes, scales, out)
-    _check("cat_mx4_dequant",
-           lib().cat_mx4_dequant(pc, ps, n, d, po, _dtype_code(out), _stream_ptr(stream)))
+    _mx4_shapes(codes, scales, n, d)
+    st = _launch_stream(stream, codes, scales, out)
+    _check("cat_mx4_dequant", lib().cat_mx4_dequant(pc, ps, n, d, po, _dtype_codes[out.dtype], st))
 
 
 def cat_mx4_linear(codes_x, scales_x, codes_w, scales_w, y, stream=None):
@@ -651,14 +661,17 @@ def cat_mx4_linear(codes_x, scales_x, codes_w, scales_w, y, stream=None):
     if codes_x.dim() != 2 or codes_w.dim() != 2:
         raise ValueError("codes_x and codes_w must be 2-D")
     n, half = codes_x.shape
-    d_out = codes_w.shape[0]
-    _mx4_shapes(codes_x, scales_x, (n,), 2 * half, "codes_x", "scales_x")
-    _mx4_shapes(codes_w, scales_w, (d_out,), 2 * half, "codes_w", "scales_w")
+    d_out, half_w = codes_w.shape
+    blocks = half >> 4
+    _mx4_blocks(2 * half)
+    if half_w != half:
+        raise ValueError(f"codes_w has shape {tuple(codes_w.shape)}, expected {(d_out, half)}")
+    _shape(scales_x, (n, blocks), "scales_x")
+    _shape(scales_w, (d_out, blocks), "scales_w")
     _shape(y, (n, d_out), "y")
-    _one_device(stream, codes_x, scales_x, codes_w, scales_w, y)
+    st = _launch_stream(stream, codes_x, scales_x, codes_w, scales_w, y)
     _check("cat_mx4_linear",
-           lib().cat_mx4_linear(pcx, psx, pcw, psw, n, 2 * half, d_out, py, _dtype_code(y),
-                                _stream_ptr(stream)))
+           lib().cat_mx4_linear(pcx, psx, pcw, psw, n, 2 * half, d_out, py, _dtype_codes[y.dtype], st))
 
 
 def cat_mx4_linear_grouped(codes_x, scales_x, offsets, codes_w, scales_w, y, row_ids=None,
@@ -667,31 +680,34 @@ def cat_mx4_linear_grouped(codes_x, scales_x, offsets, codes_w, scales_w, y, row
     1] (int32 [groups + 1]) times the weights codes_w[g] of [groups, d_out,
     d_in/2].  Row i of y takes row i of codes_x [n, d_in/2], n >= m, or row
     row_ids[i] (int32 [m])."""
-    u8 = _types("u8")
+    u8, i32 = _types("u8"), _types("i32")
     pcx = _dev_ptr(codes_x, "codes_x", u8)
     psx = _dev_ptr(scales_x, "scales_x", u8)
-    pof = _dev_ptr(offsets, "offsets", _types("i32"))
+    pof = _dev_ptr(offsets, "offsets", i32)
     pcw = _dev_ptr(codes_w, "codes_w", u8)
     psw = _dev_ptr(scales_w, "scales_w", u8)
-    pid = _dev_ptr(row_ids, "row_ids", _types("i32"), allow_none=True)
+    pid = _dev_ptr(row_ids, "row_ids", i32, allow_none=True)
     py = _dev_ptr(y, "y", _types("float"))
     if codes_x.dim() != 2 or codes_w.dim() != 3 or y.dim() != 2:
         raise ValueError("codes_x and y must be 2-D, codes_w 3-D")
     n, half = codes_x.shape
-    groups, d_out, _ = codes_w.shape
-    m = y.shape[0]
-    _mx4_shapes(codes_x, scales_x, (n,), 2 * half, "codes_x", "scales_x")
-    _mx4_shapes(codes_w, scales_w, (groups, d_out), 2 * half, "codes_w", "scales_w")
+    groups, d_out, half_w = codes_w.shape
+    m, blocks = y.shape[0], half >> 4
+    _mx4_blocks(2 * half)
+    if half_w != half:
+        raise ValueError(f"codes_w has shape {tuple(codes_w.shape)}, expected {(groups, d_out, half)}")
+    _shape(scales_x, (n, blocks), "scales_x")
+    _shape(scales_w, (groups, d_out, blocks), "scales_w")
     _shape(y, (m, d_out), "y")
     _numel(offsets, groups + 1, "offsets")
-    if pid is not None:
+    if row_ids is not None:
         _numel(row_ids, m, "row_ids")
     elif n < m:
         raise ValueError(f"y has {m} rows, codes_x only {n}, and there are no row_ids")
-    _one_device(stream, codes_x, scales_x, offsets, codes_w, scales_w, y, row_ids)
+    st = _launch_stream(stream, codes_x, scales_x, offsets, codes_w, scales_w, y, row_ids)
     _check("cat_mx4_linear_grouped",
            lib().cat_mx4_linear_grouped(pcx, psx, n, pid, m, pof, groups, pcw, psw, 2 * half, d_out,
-                                        py, _dtype_code(y), _stream_ptr(stream)))
+                                        py, _dtype_codes[y.dtype], st))
 
 
 def cat_sqnr_workspace_bytes(count: int) -> int:
