@@ -20,6 +20,7 @@
 //   6.5 us, 257 x 14336 -> 4096 29 us, 1000 x 4096 -> 4096 20 us, 8192 x 4096
 //   -> 14336 228 to 245 us (3.9 to 4.2 PFLOP/s); 128 rows of 64 experts 2048
 //   -> 1024 10 us, 16384 rows of 8 uneven experts 14336 -> 4096 520 us (3.7).
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -376,19 +377,22 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
 }
 
 // The same with whole cache lines, for rows of at least 512 elements: a chunk
-// is 256 elements, 128 bytes of every row (8 rows a copy), and 16 bytes that
-// hold its 8 scale bytes (64 rows a copy).  Every copy costs a CU about the
-// same, and copies of whole lines reach almost twice the rate of 64-byte
-// pieces.  Wave w of W takes the w-th part of the chunks, in order.
+// is 256 elements, 128 bytes of every row (8 rows a copy).  Copies of whole
+// lines reach almost twice the rate of 64-byte pieces, and what a copy costs
+// grows with the rows it touches: scale bytes therefore come 32 of a row at a
+// time (32 rows a copy), which serve four chunks.  Sixteen for every chunk, 64
+// rows a copy, took up to a third of the time (257 x 14336 -> 4096 29 us).
+// Wave w of W takes the w-th part of the chunks, in order.
 //
 // EX: d_in % 512 == 0, so that scale pieces are whole 16 bytes at multiples of
-// 16 of their row.  Otherwise a piece begins at the dword that holds its
-// chunk's first byte, moved back where it would pass the buffer's last dword,
-// and a lane finds its bytes in it; units past a row's end count as zero with
-// scale 1.
-constexpr int ln_stage_bytes(int a, int b) { return (2 * (a + b) + (a + b + 3) / 4) * 1024; }
-constexpr int ln_wave_bytes(int a, int b, int d, int w) {
-    return mx4_wave_bytes(a, b, w, d * ln_stage_bytes(a, b));
+// 16 of their row.  Otherwise the 32 bytes serve three chunks and begin at the
+// dword that holds the first one's first byte; each half of them is moved back
+// where it would pass the buffer's last dword, and a lane finds its bytes in
+// it.  Units past a row's end count as zero with scale 1.
+constexpr int ln_scale_bytes(int a, int b) { return (a + b + 1) / 2 * 1024; }
+constexpr int ln_stage_bytes(int a, int b) { return 2 * (a + b) * 1024; }
+constexpr int ln_wave_bytes(int a, int b, int d, int w) {      // as many scale buffers as chunks
+    return mx4_wave_bytes(a, b, w, d * (ln_stage_bytes(a, b) + ln_scale_bytes(a, b)));
 }
 
 template <typename Y, int A, int B, int D, int W, bool EX>
@@ -396,10 +400,12 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
                                               uint8_t (&lds)[W][ln_wave_bytes(A, B, D, W)]) {
     constexpr int BM = 16 * A, BN = 16 * B;
     constexpr int L = A + B;
-    constexpr int SC = (L + 3) / 4;        // scale copies per chunk
-    constexpr int COPIES = 2 * L + SC;
-    static_assert(COPIES * (D - 1) < 64, "copies in flight must fit the vmcnt range");
-    constexpr int kScaleAt = 2 * L * 1024, kStageBytes = ln_stage_bytes(A, B);
+    constexpr int SC = (L + 1) / 2;        // scale copies per window
+    constexpr int P = EX ? 4 : 3;          // chunks per window of scale bytes
+    constexpr int COPIES = 2 * L;          // per chunk, and SC before a window's first
+    static_assert((COPIES + SC) * D < 64, "copies in flight must fit the vmcnt range");
+    constexpr int kStageBytes = ln_stage_bytes(A, B), kScaleBytes = ln_scale_bytes(A, B);
+    constexpr int kScaleAt = D * kStageBytes;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int l16 = lane & 15, q = lane >> 4;
@@ -437,10 +443,13 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
         const int64_t bytes = (i < BM ? static_cast<int64_t>(a.n) : static_cast<int64_t>(a.groups) * a.d_out) * sb;
         return first + static_cast<uint64_t>((bytes - 1) & ~int64_t{3}) - 12;
     };
-    uint64_t ssrc[SC], smost[SC];          // of row 64 g + lane
+    // Copy g of a window: 32 bytes of rows 32 g .. 32 g + 31, half u of row r
+    // at slot 2 r + (u ^ ((r >> 3) & 1)).
+    const uint32_t su = 16u * static_cast<uint32_t>((lane & 1) ^ ((lane >> 4) & 1));
+    uint64_t ssrc[SC], smost[SC];
 #pragma unroll
     for (int g = 0; g < SC; ++g) {
-        const int i = 64 * g + lane < 16 * L ? 64 * g + lane : 16 * L - 1;
+        const int i = 32 * g + (lane >> 1) < 16 * L ? 32 * g + (lane >> 1) : 16 * L - 1;
         ssrc[g] = scale_row(i);
         if (!EX) {
             ssrc[g] &= ~uint64_t{3};
@@ -448,14 +457,28 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
         }
     }
     const uint32_t ring = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds_addr(&lds[wave][0])));
+    // the first window begins at an even chunk where its pieces are to be aligned
+    const int w0_chunk = EX ? c0 & ~1 : c0;
+    int iw = w0_chunk, ik = c0 - w0_chunk, ib = 0;         // next chunk's window, its place there, buffer
     auto issue = [&](int i, int st) {      // the wave's i-th chunk
         const uint32_t at = ring + static_cast<uint32_t>(st * kStageBytes);
         const int c = c0 + i;
+        if (i == 0 || ik == 0) {
+            const uint32_t to = static_cast<uint32_t>(
+                __builtin_amdgcn_readfirstlane(static_cast<int>(ring) + kScaleAt + ib * kScaleBytes));
 #pragma unroll
-        for (int g = 0; g < SC; ++g) {
-            uint64_t p = ssrc[g] + static_cast<uint32_t>(EX ? (c >> 1) * 16 : c * 8);
-            if (!EX) p = p < smost[g] ? p : smost[g];
-            mx4_copy16(reinterpret_cast<const uint8_t*>(p), at + kScaleAt + g * 1024u);
+            for (int g = 0; g < SC; ++g) {
+                uint32_t off = static_cast<uint32_t>(iw) * 8u + su;
+                if (EX) off = off < sb ? off : sb - 16u;           // past the row's end: any piece of it
+                uint64_t p = ssrc[g] + off;
+                if (!EX) p = p < smost[g] ? p : smost[g];
+                mx4_copy16(reinterpret_cast<const uint8_t*>(p), to + g * 1024u);
+            }
+        }
+        if (++ik == P) {
+            ik = 0;
+            iw += P;
+            ib = D > 1 ? ib ^ 1 : 0;
         }
         uint32_t col[2];                   // of even and odd copies
 #pragma unroll
@@ -469,8 +492,9 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
         for (int g = 0; g < 2 * A; ++g) mx4_copy16(src_x[g] + col[g & 1], at + g * 1024u);
     };
     const int at0 = 16 * (8 * l16 + (q ^ (l16 >> 1))), at1 = at0 ^ 64;
-    // general rows: a lane's scale byte of chunk c lies 8 c - max(8 c, far)
-    // before byte `near` of its row's piece
+    // General rows: a lane's byte of the window at chunk w, place k, is byte
+    // near + 8 k of the 32, in a half that begins 8 w + 16 u bytes behind the
+    // row's dword, or at `far` where that is less.
     int near[EX ? 1 : L], far[EX ? 1 : L];
     if (!EX) {
 #pragma unroll
@@ -481,26 +505,34 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
             far[g] = static_cast<int>(left < (1 << 30) ? left : (1 << 30));
         }
     }
+    const int swap = 16 * (l16 >> 3);
+    int rw = w0_chunk, rk = c0 - w0_chunk, rs = 0;        // as iw, ik and ib, of the next chunk read
     u32x4 f[2][L];
     int s[2][L];
     auto read = [&](int i, int st) {
         const uint8_t* at = &lds[wave][st * kStageBytes];
-        const uint8_t* sc = at + kScaleAt + 16 * l16;
+        const uint8_t* sc = &lds[wave][kScaleAt + rs * kScaleBytes + 32 * l16];
         const int c = c0 + i;
-        if (EX) sc += q + 8 * (c & 1);
 #pragma unroll
         for (int g = 0; g < L; ++g) {
-            const uint8_t* p = sc + 256 * g;
-            int i0 = 0, i1 = 4;
-            if (!EX) {                     // bytes past the row's end: any of the piece
-                const int at_byte = near[g] + (8 * c > far[g] ? 8 * c - far[g] : 0);
-                i0 = at_byte & 15;
-                i1 = (at_byte + 4) & 15;
+            const uint8_t* p = sc + 512 * g;
+            int i0 = 8 * rk + q, i1 = i0 + 4;
+            if (!EX) {                     // bytes past the row's end: any of the 32
+                i0 = near[g] + 8 * rk;
+                i1 = i0 + 4;
+                const int over0 = 8 * rw + (i0 & 16) - far[g], over1 = 8 * rw + (i1 & 16) - far[g];
+                i0 = (i0 + (over0 > 0 ? over0 : 0)) & 31;
+                i1 = (i1 + (over1 > 0 ? over1 : 0)) & 31;
             }
-            s[0][g] = p[i0];
-            s[1][g] = p[i1];
+            s[0][g] = p[i0 ^ swap];
+            s[1][g] = p[i1 ^ swap];
             f[0][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at0);
             f[1][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at1);
+        }
+        if (++rk == P) {
+            rk = 0;
+            rw += P;
+            rs = D > 1 ? rs ^ 1 : 0;
         }
         if (!EX && c == nk - 1) {          // units past the row's end
 #pragma unroll
@@ -1147,11 +1179,25 @@ static double split_cost(const Mx4Args& a, const SmallTile& t, int cus) {
     return std::ceil(tiles / cus) * (10.0 * ((a.d_in + 127) / 128) * copies + 50.0 * t.a * t.b + 1200.0);
 }
 
+// CUs of the current device, asked once a device: the question takes 0.3 us of
+// a call's 4.
+static hipError_t device_cus(int& cus) {
+    constexpr int kKept = 64;
+    static std::atomic<int> kept[kKept];
+    int dev = 0;
+    hipError_t err = hipGetDevice(&dev);
+    if (err != hipSuccess) return err;
+    cus = dev < kKept ? kept[dev].load(std::memory_order_relaxed) : 0;
+    if (cus > 0) return hipSuccess;
+    err = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+    if (err == hipSuccess && dev < kKept) kept[dev].store(cus, std::memory_order_relaxed);
+    return err;
+}
+
 template <typename Y>
 static hipError_t launch(const Mx4Args& a, hipStream_t stream) {
-    int dev = 0, cus = 0;
-    hipError_t err = hipGetDevice(&dev);
-    if (err == hipSuccess) err = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+    int cus = 0;
+    const hipError_t err = device_cus(cus);
     if (err != hipSuccess) return err;
     int pick = 0;
     double best = 0.0;
