@@ -1147,23 +1147,24 @@ static double row_tiles(const Mx4Args& a, int bm) {
 
 // Estimated nanoseconds.  Small tiles: the workgroups of a CU that fit its LDS
 // and waves run together, so a CU's tiles cost their rounds at the latency of
-// the chunks of a wave (950 ns each, 570 with two in flight) or their sum at
-// the rate of its copies (14.4 ns each) and of the sums, whichever is longer.
-// Large tiles: rounds of one tile a CU, pairs and a fixed part.  Over 550
+// the chunks of a wave (585 ns each, 300 with two in flight) or their sum at
+// the rate of its copies (11.9 ns each) and of the sums, whichever is longer.
+// Large tiles: rounds of one tile a CU, pairs and a fixed part.  Over 500
 // random shapes (1 to 4096 rows, dense and by up to 128 experts, 1024 to
 // 14336 inputs, 128 to 16384 outputs) the shape with the least estimate took
-// 2.4% longer than the fastest of the nine.
+// 2.1% longer than the fastest of the nine.
 static double line_cost(const Mx4Args& a, const SmallTile& t, int cus) {
-    const int l = t.a + t.b, copies = 2 * l + (l + 3) / 4, pieces = (a.d_in + 255) / 256;
+    const int l = t.a + t.b, pieces = (a.d_in + 255) / 256;
+    const double copies = 2 * l + 0.25 * ((l + 1) / 2);
     const int wave_bytes = ln_wave_bytes(t.a, t.b, t.d, t.w);
     const int by_lds = 160 * 1024 / (wave_bytes * t.w), by_waves = (l > 5 ? 16 : 24) / t.w;
     const int together = by_lds < by_waves ? by_lds : by_waves;
     const double tiles = row_tiles(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
     const double per_cu = std::ceil(tiles / cus), rounds = std::ceil(per_cu / together);
-    const double latency = 1000.0 + (t.d == 2 ? 570.0 : 950.0) * ((pieces + t.w - 1) / t.w) + 6.0 * copies;
-    const double work = 14.4 * pieces * copies + 70.0 * t.a * t.b + 500.0;
-    const double by_work = per_cu * work + 700.0;
-    return 2000.0 + (rounds * latency > by_work ? rounds * latency : by_work);
+    const double latency = 1090.0 + (t.d == 2 ? 300.0 : 585.0) * ((pieces + t.w - 1) / t.w) + 4.0 * copies;
+    const double work = 11.9 * pieces * copies + 67.0 * t.a * t.b + 700.0;
+    const double by_work = per_cu * work + 900.0;
+    return 1600.0 + (rounds * latency > by_work ? rounds * latency : by_work);
 }
 static double tile_cost(const Mx4Args& a, int bm, int cus) {
     const int pairs = (a.d_in + 511) / 512 * 2;
