@@ -16,10 +16,11 @@
 //          PFLOP/s of the nominal 10
 //   split  rows of less than 512 elements
 // Kernel times, weights in the last-level cache (rows x inputs -> outputs):
-//   1 x 4096 -> 4096 3.4 us, 48 x 4096 -> 14336 8.6 us, 100 x 4096 -> 4096
-//   6.5 us, 257 x 14336 -> 4096 29 us, 1000 x 4096 -> 4096 20 us, 8192 x 4096
-//   -> 14336 228 to 245 us (3.9 to 4.2 PFLOP/s); 128 rows of 64 experts 2048
-//   -> 1024 10 us, 16384 rows of 8 uneven experts 14336 -> 4096 520 us (3.7).
+//   1 x 4096 -> 4096 3.4 us, 48 x 4096 -> 14336 7.7 us, 100 x 4096 -> 4096
+//   5.8 us, 257 x 14336 -> 4096 22 us, 1000 x 4096 -> 4096 20 us, 8192 x 4096
+//   -> 14336 220 to 250 us (3.8 to 4.4 PFLOP/s); 128 rows of 64 experts 2048
+//   -> 1024 9.5 us, 16384 rows of 8 uneven experts 14336 -> 4096 506 to 530 us
+//   (3.6 to 3.8).
 #include <atomic>
 #include <cmath>
 #include <type_traits>
