@@ -14,7 +14,8 @@
  *  - Return value: CAT_OK (0) or a negative cat_status.  On failure
  *    cat_last_error() returns a thread-local message.  No C++ exception
  *    crosses this boundary.
- *  - Device calls (cov_accumulate, transform_quant, w4a4_linear, sqnr)
+ *  - Device calls (cov_accumulate, transform_quant, the linears, sqnr,
+ *    rmsnorm, mx4)
  *    take DEVICE pointers, validate their arguments on the host, enqueue
  *    kernels on `stream` (a hipStream_t passed as void*; NULL = the null
  *    stream) and return without synchronising.  Results are visible after
