@@ -11,13 +11,13 @@
 // Three forms, picked by an estimate of their times (at the end):
 //   line   few rows: small tiles, their reduction shared out among the waves of
 //          a workgroup; bound by the weights' bytes
-//   tile   many rows: 128 x 256 or 256 x 256 outputs a workgroup; bound by the
-//          matrix rate, which the power of random data holds at 6.6 to 7
+//   tile   many rows: 128 x 128, 128 x 256 or 256 x 256 outputs a workgroup;
+//          bound by the copies and the matrix rate, which the power of random data holds at 6.6 to 7
 //          PFLOP/s of the nominal 10
 //   split  rows of less than 512 elements
 // Kernel times, weights in the last-level cache (rows x inputs -> outputs):
 //   1 x 4096 -> 4096 3.4 us, 48 x 4096 -> 14336 7.7 us, 100 x 4096 -> 4096
-//   5.8 us, 257 x 14336 -> 4096 22 us, 1000 x 4096 -> 4096 20 us, 8192 x 4096
+//   5.8 us, 257 x 14336 -> 4096 22 us, 1000 x 4096 -> 4096 17 us, 8192 x 4096
 //   -> 14336 220 to 250 us (3.8 to 4.4 PFLOP/s); 128 rows of 64 experts 2048
 //   -> 1024 9.5 us, 16384 rows of 8 uneven experts 14336 -> 4096 506 to 530 us
 //   (3.6 to 3.8).
@@ -621,16 +621,18 @@ __global__ __launch_bounds__(W * kWave) void mx4_line_kernel(Mx4Args a) {
 }
 
 // ------------------------------------------------------------- large tiles
-// BM rows x 256 outputs per workgroup of four waves (2 x 2), one workgroup
-// per CU: a wave holds 128 outputs x BM/2 rows of fp32 sums (256 registers
-// with BM = 256, the accumulation half of the register file), so a fragment
-// read from LDS serves 8 matrix instructions.
+// BM rows x BN outputs per workgroup of four waves (2 x 2): a wave holds BN/2
+// outputs x BM/2 rows of fp32 sums (256 registers with 256 x 256, the
+// accumulation half of the register file), so that a fragment read from LDS
+// serves 8 matrix instructions.  One workgroup per CU, or two with 128 x 128:
+// half the copies of 64 x 64 outputs an operation where larger tiles leave CUs
+// idle (1000 x 4096 -> 4096 16.5 us; 20.3 on 64 x 64, 20.9 on 128 x 256).
 //
 // The reduction goes in pairs of stages. A stage is 128 elements, one matrix
 // step; a pair is 128 bytes of every row, a whole cache line: global -> LDS
 // copies (global_load_lds_dwordx4) of rows of 64 bytes reach 27 to 34 bytes
 // per clock and CU with all CUs reading, of 128 bytes 53.  Two pairs fit the
-// LDS.  In a stage a wave multiplies its 8 weight fragments, read during the
+// LDS.  In a stage a wave multiplies its BN/32 weight fragments, read during the
 // stage before, with token fragments that it reads three ahead of their use.
 // After the last token fragment of a pair's second stage has been read there
 // is a barrier: behind it the pair's buffer is free, the next pair but one is
@@ -647,7 +649,6 @@ __global__ __launch_bounds__(W * kWave) void mx4_line_kernel(Mx4Args a) {
 // LDS: unit u (16 bytes) of row r sits at slot 8 r + (u ^ ((r >> 1) & 7)): a
 // fragment's 16 rows at one unit fall on 16 different 16-byte bank groups.
 constexpr int kTlThreads = 256;
-constexpr int kTlN = 256;                  // outputs per tile
 constexpr int kTlUnits = 8;                // 16-byte units of a row per pair of stages
 constexpr int kTlPair = 256;               // elements of the reduction per pair
 constexpr int kTlGroupM = 4;               // row panels that are walked together
@@ -674,7 +675,7 @@ __device__ __forceinline__ int mx4_row_tiles(const Mx4Args& a) {
 // One matrix step with scale byte S of sw and sx, the sum in place in the
 // accumulation registers.  Written as an instruction because a wave's sums
 // fill that half of the register file: left to the builtin, they are moved
-// back and forth between the halves.  A sum is used again no sooner than 32
+// back and forth between the halves.  A sum is used again no sooner than 16
 // steps later, so the steps need no waits among each other.
 template <int S>
 __device__ __forceinline__ void mx4_mfma_acc(u32x4 a, u32x4 b, f32x4& acc, int sw, int sx) {
@@ -690,17 +691,18 @@ __device__ __forceinline__ void mx4_mfma_acc(u32x4 a, u32x4 b, f32x4& acc, int s
 #undef CAT_MFMA
 }
 
-template <typename Y, int BM, bool EX>
-__global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
-    constexpr int IO = 8;                  // 16-output fragments of a wave
+template <typename Y, int BM, int BN, bool EX>
+__global__ __launch_bounds__(kTlThreads, BN == 128 ? 2 : 1) void mx4_tile_kernel(Mx4Args a) {
+    constexpr int IO = BN / 32;            // 16-output fragments of a wave
     constexpr int IT = BM / 32;            // 16-row fragments of a wave
-    constexpr int ROWS = kTlN + BM;        // LDS rows: weights, then tokens
-    constexpr int LW = kTlN / 32, LX = BM / 32;     // copies a wave and pair
+    constexpr int ROWS = BN + BM;          // LDS rows: weights, then tokens
+    constexpr int LW = BN / 32, LX = BM / 32;     // copies a wave and pair
     constexpr int NL = LW + LX, NM = IO * IT;
     constexpr int XB = 4;                  // token fragments in registers
+    constexpr int WN = BN / 2, LPR = BN / 16;       // outputs of a wave, lanes that store a row of them
     __shared__ __attribute__((aligned(16))) u32x4 codes[2][ROWS * kTlUnits];
     __shared__ __attribute__((aligned(16))) u32x4 scales[2][ROWS];
-    __shared__ __attribute__((aligned(16))) u32x4 outs[kTlThreads / kWave][256];
+    __shared__ __attribute__((aligned(16))) u32x4 outs[kTlThreads / kWave][BN];
 
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -714,7 +716,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     // them in turn) walks one contiguous range, kTlGroupM row panels at a
     // time: the workgroups of an XCD share panels in its L2.
     const int tiles_m = __builtin_amdgcn_readfirstlane(mx4_row_tiles<BM>(a));
-    const int tiles_n = (a.d_out + kTlN - 1) / kTlN;
+    const int tiles_n = (a.d_out + BN - 1) / BN;
     const int64_t T = static_cast<int64_t>(tiles_m) * tiles_n;
     const int64_t per_xcd = (T + kMxXcd - 1) / kMxXcd;
     const int64_t wg_per_xcd = gridDim.x / kMxXcd;
@@ -734,7 +736,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         t.group = __builtin_amdgcn_readfirstlane(r.group);
         t.first = __builtin_amdgcn_readfirstlane(r.first);
         t.end = __builtin_amdgcn_readfirstlane(r.end);
-        t.n0 = in / gm * kTlN;
+        t.n0 = in / gm * BN;
         return true;
     };
 
@@ -756,7 +758,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         const int64_t w0 = static_cast<int64_t>(lt.group) * a.d_out + lt.n0;
         base_w = a.cw + w0 * rb;
         base_sw = a.ew + w0 * sb;
-        const int left_w = a.d_out - lt.n0 < kTlN ? a.d_out - lt.n0 : kTlN;
+        const int left_w = a.d_out - lt.n0 < BN ? a.d_out - lt.n0 : BN;
         const int left_x = lt.end - lt.first < BM ? lt.end - lt.first : BM;
         const uint32_t in_row = EX ? unit : 0u;
         // rows past the end read the last one (their results are not stored)
@@ -802,7 +804,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         // general rows: past the end any unit of the row
         const uint32_t at = EX ? 0u : (col + unit < rb ? col + unit : 0u);
         if (j < LW) mx4_copy16(base_w + (EX ? col : 0u), off_w[j] + at, dst + static_cast<uint32_t>(j) * 4096u);
-        else mx4_copy16(base_x + (EX ? col : 0u), off_x[j - LW] + at, dst + kTlN * 128u + static_cast<uint32_t>(j - LW) * 4096u);
+        else mx4_copy16(base_x + (EX ? col : 0u), off_x[j - LW] + at, dst + BN * 128u + static_cast<uint32_t>(j - LW) * 4096u);
     };
     uint32_t load_super = 0;               // byte offset of the cursor's scale buffer
     // General rows: the 16 bytes lie in the five dwords from the one that holds
@@ -812,14 +814,16 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     auto load_scales = [&]() {             // before the codes of an even pair
         const uint32_t dst = lds_scales + load_super, col = static_cast<uint32_t>(ls) * 8u;
         if (EX) {
-            mx4_copy16(base_sw + col, off_sw, dst);
-            if (BM == 256 || wave < BM / 64) mx4_copy16(base_sx + col, off_sx, dst + kTlN * 16u);
+            if (BN == 256 || wave < BN / 64) mx4_copy16(base_sw + col, off_sw, dst);
+            if (BM == 256 || wave < BM / 64) mx4_copy16(base_sx + col, off_sx, dst + BN * 16u);
         } else {
             const uint32_t w = (off_sw & ~3u) + col, x = (off_sx & ~3u) + col;
-            mx4_copy16(base_sw, w < most_sw ? w : most_sw, dst);
-            mx4_copy4(base_sw, w + 4 < most_sw ? w + 16 : most_sw + 12, lds_fifth);
+            if (BN == 256 || wave < BN / 64) {
+                mx4_copy16(base_sw, w < most_sw ? w : most_sw, dst);
+                mx4_copy4(base_sw, w + 4 < most_sw ? w + 16 : most_sw + 12, lds_fifth);
+            }
             if (BM == 256 || wave < BM / 64) {
-                mx4_copy16(base_sx, x < most_sx ? x : most_sx, dst + kTlN * 16u);
+                mx4_copy16(base_sx, x < most_sx ? x : most_sx, dst + BN * 16u);
                 mx4_copy4(base_sx, x + 4 < most_sx ? x + 16 : most_sx + 12, lds_fifth + 256u);
             }
         }
@@ -832,7 +836,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         if (static_cast<uint32_t>(pair) * 128u + unit < rb) return;
 #pragma unroll
         for (int j = 0; j < LX; ++j)
-            codes[buf][kTlN * kTlUnits + (4 * j + wave) * kWave + lane] = u32x4{0u, 0u, 0u, 0u};
+            codes[buf][BN * kTlUnits + (4 * j + wave) * kWave + lane] = u32x4{0u, 0u, 0u, 0u};
     };
 
     // ---- fragments
@@ -840,8 +844,8 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     int sw[IO], sx[IT];
     // lane (l16, q) reads row l16, unit 4 (stage % 2) + q
     const int at0 = l16 * kTlUnits + (q ^ (l16 >> 1)), at1 = at0 ^ 4;
-    const u32x4* const rd_w = &codes[0][wo * 128 * kTlUnits];
-    const u32x4* const rd_x = &codes[0][(kTlN + wt * (BM / 2)) * kTlUnits];
+    const u32x4* const rd_w = &codes[0][wo * WN * kTlUnits];
+    const u32x4* const rd_x = &codes[0][(BN + wt * (BM / 2)) * kTlUnits];
     auto frag_at = [&](int st, int i) {    // stage 0 .. 3: pair st / 2, half st % 2
         return (st / 2) * (ROWS * kTlUnits) + i * 16 * kTlUnits + (st % 2 ? at1 : at0);
     };
@@ -883,12 +887,12 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
     auto turn_scales = [&](int pair) {     // of this pair and the next
         u32x4* const p = &scales[0][turn_super + 64 * wave + lane];
         const uint32_t* const fifth = reinterpret_cast<const uint32_t*>(&outs[wave][0]) + lane;
-        turn(p, fifth, off_sw, most_sw, pair);
-        if (BM == 256 || wave < BM / 64) turn(p + kTlN, fifth + kWave, off_sx, most_sx, pair);
+        if (BN == 256 || wave < BN / 64) turn(p, fifth, off_sw, most_sw, pair);
+        if (BM == 256 || wave < BM / 64) turn(p + BN, fifth + kWave, off_sx, most_sx, pair);
         turn_super ^= ROWS;
     };
-    const int* const rd_sw = reinterpret_cast<const int*>(&scales[0][wo * 128 + l16]) + q;
-    const int* const rd_sx = reinterpret_cast<const int*>(&scales[0][kTlN + wt * (BM / 2) + l16]) + q;
+    const int* const rd_sw = reinterpret_cast<const int*>(&scales[0][wo * WN + l16]) + q;
+    const int* const rd_sx = reinterpret_cast<const int*>(&scales[0][BN + wt * (BM / 2) + l16]) + q;
     uint32_t read_super = 0;
     auto read_sw = [&](int i) { sw[i] = rd_sw[read_super + 64 * i]; };
     auto read_sx = [&](int j) { sx[j] = rd_sx[read_super + 64 * j]; };
@@ -901,11 +905,11 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
             for (int j = 0; j < IT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     };
 
-    // Accumulator (i, j) holds outputs 128 wo + 16 i + 4 q + e of row (BM/2) wt
+    // Accumulator (i, j) holds outputs WN wo + 16 i + 4 q + e of row (BM/2) wt
     // + 16 j + l16.  Sixteen rows at a time pass through LDS of the wave's own
-    // (16-byte unit u of row r at u ^ r), so that 16 lanes store 256
-    // contiguous bytes of a row: stored from the accumulators, pieces of 32
-    // bytes, a prefill's y took 68 us of 289.
+    // (16-byte unit u of row r at u ^ (r % LPR)), so that LPR lanes store 256
+    // (128 with BN = 128) contiguous bytes of a row: stored from the
+    // accumulators, pieces of 32 bytes, a prefill's y took 68 us of 289.
     u32x4* const out_lds = &outs[wave][0];
     // FULL: all of the wave's outputs exist, and rows are addressed by 32-bit
     // offsets from its first one.
@@ -927,11 +931,13 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
             return v;
         };
         constexpr int PER = 16 / sizeof(Y);            // outputs of a unit
-        constexpr int PARTS = sizeof(Y) == 4 ? 2 : 1;  // 256-byte pieces of a wave's row
-        const int rows = t.end - t.first - wt * (BM / 2), cols = a.d_out - t.n0 - wo * 128;
-        Y* const yw = static_cast<Y*>(a.y) + static_cast<int64_t>(t.first + wt * (BM / 2)) * a.d_out + t.n0 + wo * 128;
+        constexpr int PARTS = sizeof(Y) == 4 ? 2 : 1;  // pieces of a wave's row, LPR units each
+        constexpr int RPL = kWave / LPR;               // rows a store
+        const int lr = el / LPR, lu = el % LPR;
+        const int rows = t.end - t.first - wt * (BM / 2), cols = a.d_out - t.n0 - wo * WN;
+        Y* const yw = static_cast<Y*>(a.y) + static_cast<int64_t>(t.first + wt * (BM / 2)) * a.d_out + t.n0 + wo * WN;
         const uint32_t pitch = static_cast<uint32_t>(a.d_out) * sizeof(Y);
-        const uint32_t at = static_cast<uint32_t>(q) * pitch + static_cast<uint32_t>(l16) * 16u;
+        const uint32_t at = static_cast<uint32_t>(lr) * pitch + static_cast<uint32_t>(lu) * 16u;
 #pragma unroll
         for (int j = 0; j < IT; ++j) {
 #pragma unroll
@@ -941,23 +947,26 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
                     const int i = h * (IO / PARTS) + ii;
                     const float v0 = sum(i, j, 0), v1 = sum(i, j, 1), v2 = sum(i, j, 2), v3 = sum(i, j, 3);
                     if constexpr (sizeof(Y) == 4) {
-                        out_lds[l16 * 16 + ((4 * ii + q) ^ l16)] =
+                        out_lds[l16 * LPR + ((4 * ii + q) ^ (l16 % LPR))] =
                             u32x4{__float_as_uint(v0), __float_as_uint(v1), __float_as_uint(v2), __float_as_uint(v3)};
                     } else {
-                        reinterpret_cast<u32x2*>(&out_lds[l16 * 16 + ((2 * ii + (q >> 1)) ^ l16)])[q & 1] =
+                        reinterpret_cast<u32x2*>(&out_lds[l16 * LPR + ((2 * ii + (q >> 1)) ^ (l16 % LPR))])[q & 1] =
                             u32x2{pack_bf16(v0, v1), pack_bf16(v2, v3)};
                     }
                 }
-                u32x4 v[4];
+                u32x4 v[16 / RPL];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = out_lds[(4 * r + q) * 16 + (l16 ^ (4 * r + q))];
-                const int c = h * (128 / PARTS) + l16 * PER;
+                for (int r = 0; r < 16 / RPL; ++r) {
+                    const int row = RPL * r + lr;
+                    v[r] = out_lds[row * LPR + (lu ^ (row % LPR))];
+                }
+                const int c = h * (WN / PARTS) + lu * PER;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * j + 4 * r + q;            // 16 lanes a row
+                for (int r = 0; r < 16 / RPL; ++r) {
+                    const int row = 16 * j + RPL * r + lr;
                     // 16-byte stores may start at any byte here
                     if constexpr (FULL) {
-                        char* const base = reinterpret_cast<char*>(yw + h * (128 / PARTS)) + static_cast<uint64_t>(16 * j + 4 * r) * pitch;
+                        char* const base = reinterpret_cast<char*>(yw + h * (WN / PARTS)) + static_cast<uint64_t>(16 * j + RPL * r) * pitch;
                         __builtin_memcpy(base + at, &v[r], 16);
                     } else if (row < rows && c < cols) {
                         Y* const y = yw + static_cast<int64_t>(row) * a.d_out + c;
@@ -977,7 +986,7 @@ __global__ __launch_bounds__(kTlThreads, 1) void mx4_tile_kernel(Mx4Args a) {
         }
     };
     auto store = [&](const Tile& t) {
-        const bool full = t.end - t.first - wt * (BM / 2) >= BM / 2 && a.d_out - t.n0 - wo * 128 >= 128;
+        const bool full = t.end - t.first - wt * (BM / 2) >= BM / 2 && a.d_out - t.n0 - wo * WN >= WN;
         if (full && a.d_out < (1 << 22)) store_as(t, std::true_type{});
         else store_as(t, std::false_type{});
     };
@@ -1130,10 +1139,10 @@ static hipError_t launch_line(const Mx4Args& a, int tile, hipStream_t stream) {
     return hipGetLastError();
 }
 
-template <typename Y, int BM, bool EX>
+template <typename Y, int BM, int BN, bool EX>
 static hipError_t launch_tiles(const Mx4Args& a, int cus, hipStream_t stream) {
-    const unsigned grid = static_cast<unsigned>(cus >= kMxXcd ? cus / kMxXcd * kMxXcd : kMxXcd);
-    mx4_tile_kernel<Y, BM, EX><<<grid, kTlThreads, 0, stream>>>(a);
+    const unsigned grid = static_cast<unsigned>(cus >= kMxXcd ? cus / kMxXcd * kMxXcd : kMxXcd) * (BN == 128 ? 2 : 1);
+    mx4_tile_kernel<Y, BM, BN, EX><<<grid, kTlThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -1148,12 +1157,13 @@ static double row_tiles(const Mx4Args& a, int bm) {
 
 // Estimated nanoseconds.  Small tiles: the workgroups of a CU that fit its LDS
 // and waves run together, so a CU's tiles cost their rounds at the latency of
-// the chunks of a wave (585 ns each, 300 with two in flight) or their sum at
-// the rate of its copies (11.9 ns each) and of the sums, whichever is longer.
-// Large tiles: rounds of one tile a CU, pairs and a fixed part.  Over 500
-// random shapes (1 to 4096 rows, dense and by up to 128 experts, 1024 to
-// 14336 inputs, 128 to 16384 outputs) the shape with the least estimate took
-// 2.1% longer than the fastest of the nine.
+// the chunks of a wave (580 ns each, 360 with two in flight) or their sum at
+// the rate of its copies (13.9 ns each) and of the sums, whichever is longer.
+// Large tiles: rounds, pairs and a fixed part; 128 x 128 outputs run two a CU,
+// a pair of both in 1.2 us where one alone takes 0.64.  Over 700 random shapes
+// (1 to 4096 rows, dense and by up to 128 experts, 1024 to 14336 inputs, 128 to
+// 16384 outputs) the shape with the least estimate took 2.5% longer than the
+// fastest of the ten.
 static double line_cost(const Mx4Args& a, const SmallTile& t, int cus) {
     const int l = t.a + t.b, pieces = (a.d_in + 255) / 256;
     const double copies = 2 * l + 0.25 * ((l + 1) / 2);
@@ -1162,15 +1172,20 @@ static double line_cost(const Mx4Args& a, const SmallTile& t, int cus) {
     const int together = by_lds < by_waves ? by_lds : by_waves;
     const double tiles = row_tiles(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
     const double per_cu = std::ceil(tiles / cus), rounds = std::ceil(per_cu / together);
-    const double latency = 1090.0 + (t.d == 2 ? 300.0 : 585.0) * ((pieces + t.w - 1) / t.w) + 4.0 * copies;
-    const double work = 11.9 * pieces * copies + 67.0 * t.a * t.b + 700.0;
+    const double latency = 1360.0 + (t.d == 2 ? 360.0 : 580.0) * ((pieces + t.w - 1) / t.w) + 6.0 * copies;
+    const double work = 13.9 * pieces * copies + 71.0 * t.a * t.b + 570.0;
     const double by_work = per_cu * work + 900.0;
-    return 1600.0 + (rounds * latency > by_work ? rounds * latency : by_work);
+    return 1560.0 + (rounds * latency > by_work ? rounds * latency : by_work);
 }
-static double tile_cost(const Mx4Args& a, int bm, int cus) {
+static double tile_cost(const Mx4Args& a, int bm, int bn, int cus) {
     const int pairs = (a.d_in + 511) / 512 * 2;
-    const double tiles = row_tiles(a, bm) * ((a.d_out + kTlN - 1) / kTlN), rounds = std::ceil(tiles / cus);
-    return bm == 128 ? rounds * (800.0 * pairs + 8700.0) - 2400.0 : rounds * (1200.0 * pairs + 11400.0) - 3400.0;
+    const double tiles = row_tiles(a, bm) * ((a.d_out + bn - 1) / bn);
+    if (bn == 128) {
+        const double full = std::ceil(tiles / (2 * cus)) - 1.0, rest = tiles - full * 2 * cus;
+        return full * (1198.0 * pairs + 4270.0) + (rest > cus ? 1198.0 * pairs + 4270.0 : 640.0 * pairs + 4310.0);
+    }
+    const double rounds = std::ceil(tiles / cus);
+    return bm == 128 ? rounds * (970.0 * pairs + 5940.0) + 120.0 : rounds * (1360.0 * pairs + 8630.0) - 500.0;
 }
 // Short rows (the split kernel): all its waves together hold the whole
 // reduction, so a tile is a fixed part, its copies and its sums.  2.7% over
@@ -1218,12 +1233,14 @@ static hipError_t launch(const Mx4Args& a, hipStream_t stream) {
     for (int i = 0; i < n; ++i) offer(i, line_cost(a, kLnTiles[i], cus));
     // the large tiles take 32-bit offsets into gathered rows
     if (!a.row_ids || static_cast<int64_t>(a.n) * (a.d_in / 2) < (int64_t{1} << 32)) {
-        offer(n, tile_cost(a, 128, cus));
-        offer(n + 1, tile_cost(a, 256, cus));
+        offer(n, tile_cost(a, 128, 128, cus));
+        offer(n + 1, tile_cost(a, 128, 256, cus));
+        offer(n + 2, tile_cost(a, 256, 256, cus));
     }
     const bool ex = a.d_in % 512 == 0;
-    if (pick == n) return ex ? launch_tiles<Y, 128, true>(a, cus, stream) : launch_tiles<Y, 128, false>(a, cus, stream);
-    if (pick == n + 1) return ex ? launch_tiles<Y, 256, true>(a, cus, stream) : launch_tiles<Y, 256, false>(a, cus, stream);
+    if (pick == n) return ex ? launch_tiles<Y, 128, 128, true>(a, cus, stream) : launch_tiles<Y, 128, 128, false>(a, cus, stream);
+    if (pick == n + 1) return ex ? launch_tiles<Y, 128, 256, true>(a, cus, stream) : launch_tiles<Y, 128, 256, false>(a, cus, stream);
+    if (pick == n + 2) return ex ? launch_tiles<Y, 256, 256, true>(a, cus, stream) : launch_tiles<Y, 256, 256, false>(a, cus, stream);
     return ex ? launch_line<Y, true>(a, pick, stream) : launch_line<Y, false>(a, pick, stream);
 }
 
