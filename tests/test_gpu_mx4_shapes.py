@@ -72,6 +72,42 @@ def test_scales_at_the_end_of_their_buffer(d_in, d_out, m):
         _assert_close(y, *mo.linear(cx, sx, cw, sw), d_in, f"{m + extra}x{d_in}->{d_out + extra}")
 
 
+# Sizes at which the products take 128 x 128, 128 x 256 and 256 x 256 outputs a
+# workgroup: whole and general rows, last row and output tiles partly filled,
+# outputs at 2-byte addresses; by expert with gathered rows, experts without
+# rows, and rows before the first and behind the last expert left alone.
+@pytest.mark.parametrize("n,d_in,d_out", [(700, 544, 3001), (600, 1024, 2047), (1300, 2080, 3003),
+                                          (1300, 2048, 3002), (2000, 544, 5001), (2000, 1024, 4999)])
+@pytest.mark.parametrize("grouped", [False, True])
+def test_large_tiles(n, d_in, d_out, grouped):
+    torch = torch_mod()
+    cw, sw = _codes(d_out, d_in, 3, 118, 136)
+    if not grouped:
+        cx, sx = _codes(n, d_in, 2, 118, 136)
+        ref, absum = mo.linear(cx, sx, cw, sw)
+        for dt in (torch.float32, torch.bfloat16):
+            y = torch.full((n, d_out), float("nan"), dtype=dt, device="cuda")
+            _cat().cat_mx4_linear(_dev(cx), _dev(sx), _dev(cw), _dev(sw), y)
+            _assert_close(y, ref, absum, d_in, f"{n}x{d_in}->{d_out} {dt}")
+        return
+    # the experts' weights are the same rows, rotated, so that one product
+    # holds every reference value
+    groups, shift, tokens = 4, 37, 150
+    cx, sx = _codes(tokens, d_in, 2, 118, 136)
+    full, full_abs = mo.linear(cx, sx, cw, sw)
+    cws, sws = (np.stack([np.roll(v, g * shift, 0) for g in range(groups)]) for v in (cw, sw))
+    off = np.array([5, n // 3, n // 3, n - 140, n - 3], np.int32)
+    ids = np.random.default_rng(n).integers(0, tokens, n).astype(np.int32)
+    of = np.searchsorted(off, np.arange(5, n - 3), side="right") - 1
+    ref = np.stack([np.roll(full[ids[i]], of[i - 5] * shift) for i in range(5, n - 3)])
+    absum = np.stack([np.roll(full_abs[ids[i]], of[i - 5] * shift) for i in range(5, n - 3)])
+    for dt in (torch.float32, torch.bfloat16):
+        y = torch.full((n, d_out), 7.0, dtype=dt, device="cuda")
+        _cat().cat_mx4_linear_grouped(_dev(cx), _dev(sx), _dev(off), _dev(cws), _dev(sws), y, row_ids=_dev(ids))
+        assert (y[:5] == 7).all() and (y[n - 3:] == 7).all()
+        _assert_close(y[5:n - 3], ref, absum, d_in, f"by expert {n}x{d_in}->{d_out} {dt}")
+
+
 # --------------------------------------------------------- beyond 32-bit offsets
 def _random_codes(torch, *shape):
     g = torch.Generator(device="cuda")
