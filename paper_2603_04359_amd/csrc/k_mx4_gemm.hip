@@ -461,10 +461,12 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
     // the first window begins at an even chunk where its pieces are to be aligned
     const int w0_chunk = EX ? c0 & ~1 : c0;
     int iw = w0_chunk, ik = c0 - w0_chunk, ib = 0;         // next chunk's window, its place there, buffer
-    auto issue = [&](int i, int st) {      // the wave's i-th chunk
+    // Of the wave's i-th chunk the weights and scales, the tokens, or both.
+    constexpr int kWeights = 1, kTokens = 2, kBoth = 3;
+    auto issue = [&](int i, int st, int part) {
         const uint32_t at = ring + static_cast<uint32_t>(st * kStageBytes);
         const int c = c0 + i;
-        if (i == 0 || ik == 0) {
+        if ((part & kWeights) && (i == 0 || ik == 0)) {
             const uint32_t to = static_cast<uint32_t>(
                 __builtin_amdgcn_readfirstlane(static_cast<int>(ring) + kScaleAt + ib * kScaleBytes));
 #pragma unroll
@@ -476,7 +478,7 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
                 mx4_copy16(reinterpret_cast<const uint8_t*>(p), to + g * 1024u);
             }
         }
-        if (++ik == P) {
+        if ((part & kWeights) && ++ik == P) {
             ik = 0;
             iw += P;
             ib = D > 1 ? ib ^ 1 : 0;
@@ -488,9 +490,11 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
             if (!EX) col[h] = col[h] < rb ? col[h] : 0;        // past the row's end: any unit of it
         }
 #pragma unroll
-        for (int g = 0; g < 2 * B; ++g) mx4_copy16(base_w, src_w[g] + col[g & 1], at + (2 * A + g) * 1024u);
+        for (int g = 0; g < 2 * B; ++g)
+            if (part & kWeights) mx4_copy16(base_w, src_w[g] + col[g & 1], at + (2 * A + g) * 1024u);
 #pragma unroll
-        for (int g = 0; g < 2 * A; ++g) mx4_copy16(src_x[g] + col[g & 1], at + g * 1024u);
+        for (int g = 0; g < 2 * A; ++g)
+            if (part & kTokens) mx4_copy16(src_x[g] + col[g & 1], at + g * 1024u);
     };
     const int at0 = 16 * (8 * l16 + (q ^ (l16 >> 1))), at1 = at0 ^ 64;
     // General rows: a lane's byte of the window at chunk w, place k, is byte
@@ -510,32 +514,36 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
     int rw = w0_chunk, rk = c0 - w0_chunk, rs = 0;        // as iw, ik and ib, of the next chunk read
     u32x4 f[2][L];
     int s[2][L];
-    auto read = [&](int i, int st) {
+    auto read = [&](int i, int st, int part) {
         const uint8_t* at = &lds[wave][st * kStageBytes];
         const uint8_t* sc = &lds[wave][kScaleAt + rs * kScaleBytes + 32 * l16];
         const int c = c0 + i;
 #pragma unroll
         for (int g = 0; g < L; ++g) {
-            const uint8_t* p = sc + 512 * g;
-            int i0 = 8 * rk + q, i1 = i0 + 4;
-            if (!EX) {                     // bytes past the row's end: any of the 32
-                i0 = near[g] + 8 * rk;
-                i1 = i0 + 4;
-                const int over0 = 8 * rw + (i0 & 16) - far[g], over1 = 8 * rw + (i1 & 16) - far[g];
-                i0 = (i0 + (over0 > 0 ? over0 : 0)) & 31;
-                i1 = (i1 + (over1 > 0 ? over1 : 0)) & 31;
+            if (part & kWeights) {
+                const uint8_t* p = sc + 512 * g;
+                int i0 = 8 * rk + q, i1 = i0 + 4;
+                if (!EX) {                 // bytes past the row's end: any of the 32
+                    i0 = near[g] + 8 * rk;
+                    i1 = i0 + 4;
+                    const int over0 = 8 * rw + (i0 & 16) - far[g], over1 = 8 * rw + (i1 & 16) - far[g];
+                    i0 = (i0 + (over0 > 0 ? over0 : 0)) & 31;
+                    i1 = (i1 + (over1 > 0 ? over1 : 0)) & 31;
+                }
+                s[0][g] = p[i0 ^ swap];
+                s[1][g] = p[i1 ^ swap];
             }
-            s[0][g] = p[i0 ^ swap];
-            s[1][g] = p[i1 ^ swap];
-            f[0][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at0);
-            f[1][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at1);
+            if (part & (g < A ? kTokens : kWeights)) {
+                f[0][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at0);
+                f[1][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at1);
+            }
         }
-        if (++rk == P) {
+        if ((part & kWeights) && ++rk == P) {
             rk = 0;
             rw += P;
             rs = D > 1 ? rs ^ 1 : 0;
         }
-        if (!EX && c == nk - 1) {          // units past the row's end
+        if ((part & kTokens) && !EX && c == nk - 1) {      // units past the row's end
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const bool past = 8 * c + 4 * h + q >= static_cast<int>(sb);
@@ -563,21 +571,34 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
     };
 #pragma unroll
     for (int st = 0; st < D; ++st)
-        if (st < cnt) issue(st, st);
+        if (st < cnt) issue(st, st, kBoth);
     int i = 0, st = 0;
     for (; i + D < cnt; ++i) {
         wait_vmcnt<(D - 1) * COPIES>();
         asm volatile("" ::: "memory");
-        read(i, st);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        issue(i + D, st);
+        if constexpr (A > 2) {
+            // the weights' copies leave before the tokens are read: 48 x 4096
+            // -> 14336 7.1 us, 7.6 with all of them behind all reads; with
+            // fewer fragments the second wait costs as much (64 rows on 32 x
+            // 64 outputs 8.4, 8.0)
+            read(i, st, kWeights);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            issue(i + D, st, kWeights);
+            read(i, st, kTokens);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            issue(i + D, st, kTokens);
+        } else {
+            read(i, st, kBoth);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            issue(i + D, st, kBoth);
+        }
         compute();
         st = st + 1 == D ? 0 : st + 1;
     }
     wait_vmcnt<0>();
     asm volatile("" ::: "memory");
     for (; i < cnt; ++i) {
-        read(i, st);
+        read(i, st, kBoth);
         compute();
         st = st + 1 == D ? 0 : st + 1;
     }
