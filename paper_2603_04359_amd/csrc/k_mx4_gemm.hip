@@ -16,7 +16,7 @@
 //          PFLOP/s of the nominal 10
 //   split  rows of less than 512 elements
 // Kernel times, weights in the last-level cache (rows x inputs -> outputs):
-//   1 x 4096 -> 4096 3.4 us, 48 x 4096 -> 14336 7.7 us, 100 x 4096 -> 4096
+//   1 x 4096 -> 4096 3.4 us, 48 x 4096 -> 14336 7.1 us, 100 x 4096 -> 4096
 //   5.8 us, 257 x 14336 -> 4096 22 us, 1000 x 4096 -> 4096 17 us, 8192 x 4096
 //   -> 14336 220 to 250 us (3.8 to 4.4 PFLOP/s); 128 rows of 64 experts 2048
 //   -> 1024 9.5 us, 16384 rows of 8 uneven experts 14336 -> 4096 506 to 530 us
