@@ -385,11 +385,12 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
 // rows a copy, took up to a third of the time (257 x 14336 -> 4096 29 us).
 // Wave w of W takes the w-th part of the chunks, in order.
 //
-// EX: d_in % 512 == 0, so that scale pieces are whole 16 bytes at multiples of
-// 16 of their row.  Otherwise the 32 bytes serve three chunks and begin at the
+// EX: d_in % 256 == 0, so that chunks are whole and scale bytes begin at dwords;
+// windows begin where none of their 16-byte pieces passes a row's end with its
+// first half in it.  Otherwise the 32 bytes serve three chunks and begin at the
 // dword that holds the first one's first byte; each half of them is moved back
 // where it would pass the buffer's last dword, and a lane finds its bytes in
-// it.  Units past a row's end count as zero with scale 1.
+// it; units past a row's end count as zero with scale 1.
 constexpr int ln_scale_bytes(int a, int b) { return (a + b + 1) / 2 * 1024; }
 constexpr int ln_stage_bytes(int a, int b) { return 2 * (a + b) * 1024; }
 constexpr int ln_wave_bytes(int a, int b, int d, int w) {      // as many scale buffers as chunks
@@ -458,9 +459,14 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
         }
     }
     const uint32_t ring = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds_addr(&lds[wave][0])));
-    // the first window begins at an even chunk where its pieces are to be aligned
-    const int w0_chunk = EX ? c0 & ~1 : c0;
-    int iw = w0_chunk, ik = c0 - w0_chunk, ib = 0;         // next chunk's window, its place there, buffer
+    // Whole chunks: windows begin at chunks as even or odd as the row's end.
+    // The first one begins a chunk early for that, or, at the row's start, holds
+    // one chunk alone.
+    const int odd = EX ? (c0 ^ nk) & 1 : 0;
+    const bool lone = odd && c0 == 0;
+    const int w0_chunk = lone ? 0 : c0 - odd;
+    // next chunk's window, its place there, the window's end and buffer
+    int iw = w0_chunk, ik = c0 - w0_chunk, ie = lone ? 1 : P, ib = 0;
     // Of the wave's i-th chunk the weights and scales, the tokens, or both.
     constexpr int kWeights = 1, kTokens = 2, kBoth = 3;
     auto issue = [&](int i, int st, int part) {
@@ -472,15 +478,16 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
 #pragma unroll
             for (int g = 0; g < SC; ++g) {
                 uint32_t off = static_cast<uint32_t>(iw) * 8u + su;
-                if (EX) off = off < sb ? off : sb - 16u;           // past the row's end: any piece of it
+                if (EX) off = off + 16u <= sb ? off : sb - 16u;    // past the row's end: any piece of it
                 uint64_t p = ssrc[g] + off;
                 if (!EX) p = p < smost[g] ? p : smost[g];
                 mx4_copy16(reinterpret_cast<const uint8_t*>(p), to + g * 1024u);
             }
         }
-        if ((part & kWeights) && ++ik == P) {
+        if ((part & kWeights) && ++ik == ie) {
+            iw += ie;
             ik = 0;
-            iw += P;
+            ie = P;
             ib = D > 1 ? ib ^ 1 : 0;
         }
         uint32_t col[2];                   // of even and odd copies
@@ -511,7 +518,7 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
         }
     }
     const int swap = 16 * (l16 >> 3);
-    int rw = w0_chunk, rk = c0 - w0_chunk, rs = 0;        // as iw, ik and ib, of the next chunk read
+    int rw = iw, rk = ik, re = ie, rs = 0;                 // the same of the next chunk read
     u32x4 f[2][L];
     int s[2][L];
     auto read = [&](int i, int st, int part) {
@@ -538,9 +545,10 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
                 f[1][g] = *reinterpret_cast<const u32x4*>(at + g * 2048 + at1);
             }
         }
-        if ((part & kWeights) && ++rk == P) {
+        if ((part & kWeights) && ++rk == re) {
+            rw += re;
             rk = 0;
-            rw += P;
+            re = P;
             rs = D > 1 ? rs ^ 1 : 0;
         }
         if ((part & kTokens) && !EX && c == nk - 1) {      // units past the row's end
@@ -1258,11 +1266,11 @@ static hipError_t launch(const Mx4Args& a, hipStream_t stream) {
         offer(n + 1, tile_cost(a, 128, 256, cus));
         offer(n + 2, tile_cost(a, 256, 256, cus));
     }
-    const bool ex = a.d_in % 512 == 0;
+    const bool ex = a.d_in % 512 == 0;     // of the large tiles; rows of whole chunks for the line kernel
     if (pick == n) return ex ? launch_tiles<Y, 128, 128, true>(a, cus, stream) : launch_tiles<Y, 128, 128, false>(a, cus, stream);
     if (pick == n + 1) return ex ? launch_tiles<Y, 128, 256, true>(a, cus, stream) : launch_tiles<Y, 128, 256, false>(a, cus, stream);
     if (pick == n + 2) return ex ? launch_tiles<Y, 256, 256, true>(a, cus, stream) : launch_tiles<Y, 256, 256, false>(a, cus, stream);
-    return ex ? launch_line<Y, true>(a, pick, stream) : launch_line<Y, false>(a, pick, stream);
+    return a.d_in % 256 == 0 ? launch_line<Y, true>(a, pick, stream) : launch_line<Y, false>(a, pick, stream);
 }
 
 hipError_t launch_mx4_linear(const uint8_t* cx, const uint8_t* ex, const uint8_t* cw,
