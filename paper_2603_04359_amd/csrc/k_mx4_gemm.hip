@@ -838,7 +838,9 @@ __global__ __launch_bounds__(kTlThreads, BN == 128 ? 2 : 1) void mx4_tile_kernel
     uint32_t load_super = 0;               // byte offset of the cursor's scale buffer
     // General rows: the 16 bytes lie in the five dwords from the one that holds
     // the first of them, the fifth copied to the wave's output space (which is
-    // not in use then).  At the buffer's end the 16 bytes begin earlier.
+    // not in use then; without it where rows begin at dwords).  At the buffer's
+    // end the 16 bytes begin earlier.
+    const bool fifths = sb % 4 != 0;
     const uint32_t lds_fifth = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds_addr(&outs[wave][0])));
     auto load_scales = [&]() {             // before the codes of an even pair
         const uint32_t dst = lds_scales + load_super, col = static_cast<uint32_t>(ls) * 8u;
@@ -849,11 +851,11 @@ __global__ __launch_bounds__(kTlThreads, BN == 128 ? 2 : 1) void mx4_tile_kernel
             const uint32_t w = (off_sw & ~3u) + col, x = (off_sx & ~3u) + col;
             if (BN == 256 || wave < BN / 64) {
                 mx4_copy16(base_sw, w < most_sw ? w : most_sw, dst);
-                mx4_copy4(base_sw, w + 4 < most_sw ? w + 16 : most_sw + 12, lds_fifth);
+                if (fifths) mx4_copy4(base_sw, w + 4 < most_sw ? w + 16 : most_sw + 12, lds_fifth);
             }
             if (BM == 256 || wave < BM / 64) {
                 mx4_copy16(base_sx, x < most_sx ? x : most_sx, dst + BN * 16u);
-                mx4_copy4(base_sx, x + 4 < most_sx ? x + 16 : most_sx + 12, lds_fifth + 256u);
+                if (fifths) mx4_copy4(base_sx, x + 4 < most_sx ? x + 16 : most_sx + 12, lds_fifth + 256u);
             }
         }
         load_super ^= ROWS * 16u;
