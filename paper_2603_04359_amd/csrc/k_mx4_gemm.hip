@@ -141,37 +141,21 @@ __device__ __forceinline__ void mx4_store4(Y* y, int d_out, int first, int n0, i
 }
 
 // global -> LDS copies as dma16 and dma4 of the common header (16 or 4 bytes a
-// lane, the lane's bytes at lds + 16 or 4 lane), with M0 given up instead of
-// saved: nothing else in these kernels uses it, and a copy is then three
-// instructions.  From a wave-uniform base and a 32-bit offset a lane, or from
-// an address a lane.
+// lane, the lane's bytes at lds + 16 or 4 lane), with M0 as an operand that the
+// compiler writes instead of saved and restored around each: a copy is then
+// three instructions.  From a wave-uniform base and a 32-bit offset a lane, or
+// from an address a lane.
 __device__ __forceinline__ void mx4_copy16(const uint8_t* base, uint32_t off, uint32_t lds) {
-    asm volatile(
-        "s_mov_b32 m0, %2\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds)
-        : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void mx4_copy4(const uint8_t* base, uint32_t off, uint32_t lds) {
-    asm volatile(
-        "s_mov_b32 m0, %2\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds)
-        : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void mx4_copy16(const uint8_t* p, uint32_t lds) {
-    asm volatile(
-        "s_mov_b32 m0, %1\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %0, off" ::"v"(p), "s"(lds)
-        : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void mx4_copy4(const uint8_t* p, uint32_t lds) {
-    asm volatile(
-        "s_mov_b32 m0, %1\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dword %0, off" ::"v"(p), "s"(lds)
-        : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(p), "{m0}"(lds) : "memory");
 }
 
 // -------------------------------------------------- tiles for fewer rows
