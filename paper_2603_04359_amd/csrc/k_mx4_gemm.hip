@@ -14,7 +14,8 @@
 //   tile   many rows: 128 x 128, 128 x 256 or 256 x 256 outputs a workgroup;
 //          bound by the copies and the matrix rate, which the power of random data holds at 6.6 to 7
 //          PFLOP/s of the nominal 10
-//   split  rows of less than 512 elements
+//   split  rows of less than 512 elements, a wave for each 128 of them; bound
+//          by the outputs' bytes
 // Kernel times, weights in the last-level cache (rows x inputs -> outputs):
 //   1 x 4096 -> 4096 3.4 us, 48 x 4096 -> 14336 7.1 us, 100 x 4096 -> 4096
 //   5.8 us, 257 x 14336 -> 4096 22 us, 1000 x 4096 -> 4096 17 us, 8192 x 4096
@@ -158,13 +159,12 @@ __device__ __forceinline__ void mx4_copy4(const uint8_t* p, uint32_t lds) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(p), "{m0}"(lds) : "memory");
 }
 
-// -------------------------------------------------- tiles for fewer rows
-// A workgroup of 8 waves owns 16 A rows x 16 B outputs and its waves share
-// out the reduction: wave w takes its w-th eighth of the chunks of 128
-// elements, streams them through an LDS ring of its own (D chunks of A + B
-// KiB of codes and their scale bytes, global -> LDS copies, no barriers), and
-// the 8 partial sums are added in LDS in the waves' order.  A tile's weights
-// are then read by 8 waves at once, so a few rows still keep HBM busy.
+// -------------------------------------------------------- tiles for short rows
+// Rows of less than 512 elements, up to four chunks of 128: a workgroup owns 16
+// A rows x 16 B outputs and has a wave for each chunk, which copies its A + B
+// KiB of codes and their scale bytes to LDS (global -> LDS copies, all in
+// flight at once) and multiplies them; the waves' partial sums are then added
+// in LDS in the chunks' order.
 //
 // A chunk's copies: 16 rows x 64 bytes of codes per fragment (four lanes on
 // 64 contiguous bytes; unit u of row r at slot 4 r + (u ^ ((r >> 2) & 3))),
@@ -174,27 +174,28 @@ __device__ __forceinline__ void mx4_copy4(const uint8_t* p, uint32_t lds) {
 // end are read with it, never used) and a lane picks its byte, at a place
 // that depends on its row only.  Units past a row's end count as zero with
 // scale 1.
-constexpr int kSpWaves = 8;
-constexpr int kSpThreads = kSpWaves * kWave;
+//
+// 8192 x 256 -> 4096 27 us and 1000 x 480 -> 4096 8.5; with eight waves of
+// which half or more had no chunk, and a ring for each, 92 and 16.
+constexpr int kSpWaves = 4;                // at most
+constexpr int kSpRow = 512;                // elements that a row has less of
+static_assert(kSpRow == 128 * kSpWaves, "a wave for each chunk, none without");
 
 // Accumulators whose partial sums are added at a time: one per wave.
 constexpr int mx4_round(int a, int b, int w) { return a * b < w ? a * b : w; }
-// LDS of a wave: its ring, later its partial sums of a round.
+// LDS of a wave: its copies, later its partial sums of a round.
 constexpr int mx4_wave_bytes(int a, int b, int w, int ring) {
     return ring > mx4_round(a, b, w) * 1024 ? ring : mx4_round(a, b, w) * 1024;
 }
-constexpr int sp_stage_bytes(int a, int b, bool aligned) {
-    return (a + b) * 1024 + (a + b + 3) / 4 * 256 * (aligned ? 1 : 2);
-}
-constexpr int sp_wave_bytes(int a, int b, int d, bool aligned) {
-    return mx4_wave_bytes(a, b, kSpWaves, d * sp_stage_bytes(a, b, aligned));
+constexpr int sp_wave_bytes(int a, int b, bool aligned) {
+    return mx4_wave_bytes(a, b, kSpWaves, (a + b) * 1024 + (a + b + 3) / 4 * 256 * (aligned ? 1 : 2));
 }
 
-// Adds the W waves' partial sums of a tile, in the waves' order, through LDS
-// and stores them.
+// Adds the partial sums of the workgroup's waves (W at most) in the waves'
+// order through LDS and stores them.
 template <typename Y, int A, int B, int W, int BYTES>
-__device__ __forceinline__ void mx4_join(const Mx4Args& a, const Mx4Rows& r, int n0,
-                                         uint8_t (&lds)[W][BYTES], const f32x4 (&acc)[A][B]) {
+__device__ __forceinline__ void mx4_join(const Mx4Args& a, const Mx4Rows& r, int n0, int waves,
+                                         uint8_t (*lds)[BYTES], const f32x4 (&acc)[A][B]) {
     constexpr int RT = mx4_round(A, B, W), ROUNDS = (A * B + RT - 1) / RT;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -208,12 +209,14 @@ __device__ __forceinline__ void mx4_join(const Mx4Args& a, const Mx4Rows& r, int
             if (tl < A * B) reinterpret_cast<f32x4*>(&lds[wave][0])[t * kWave + lane] = acc[tl / B][tl % B];
         }
         __syncthreads();
-        const int tl = rd * RT + wave;
-        if (wave < RT && tl < A * B) {
-            f32x4 v = reinterpret_cast<const f32x4*>(&lds[0][0])[wave * kWave + lane];
+        for (int t = wave; t < RT; t += waves) {
+            const int tl = rd * RT + t;
+            if (tl >= A * B) break;
+            f32x4 v = reinterpret_cast<const f32x4*>(&lds[0][0])[t * kWave + lane];
 #pragma unroll
             for (int w = 1; w < W; ++w) {
-                const f32x4 p = reinterpret_cast<const f32x4*>(&lds[w][0])[wave * kWave + lane];
+                if (w >= waves) break;
+                const f32x4 p = reinterpret_cast<const f32x4*>(&lds[w][0])[t * kWave + lane];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += p[e];
             }
@@ -224,22 +227,19 @@ __device__ __forceinline__ void mx4_join(const Mx4Args& a, const Mx4Rows& r, int
     }
 }
 
-template <typename Y, int A, int B, int D, bool ALN>
+template <typename Y, int A, int B, bool ALN>
 __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& r, int n0,
-                                               uint8_t (&lds)[kSpWaves][sp_wave_bytes(A, B, D, ALN)]) {
+                                               uint8_t (*lds)[sp_wave_bytes(A, B, ALN)]) {
     constexpr int BM = 16 * A, BN = 16 * B;
     constexpr int L = A + B;               // code copies per chunk
     constexpr int SC = (L + 3) / 4;        // scale copies per chunk and dword
-    constexpr int COPIES = L + SC * (ALN ? 1 : 2);
-    static_assert(COPIES * (D - 1) < 64, "copies in flight must fit the vmcnt range");
-    constexpr int kScaleAt = L * 1024;     // bytes in a ring stage
-    constexpr int kStageBytes = sp_stage_bytes(A, B, ALN);
+    constexpr int kScaleAt = L * 1024;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int l16 = lane & 15, q = lane >> 4;
     const uint32_t rb = static_cast<uint32_t>(a.d_in) / 2;
     const uint32_t sb = static_cast<uint32_t>(a.d_in) / 32;
-    const int nk = (a.d_in + 127) / 128;
+    const int chunk = wave;
     const int rows_x = r.end - r.first < BM ? r.end - r.first : BM;
     const int rows_w = a.d_out - n0 < BN ? a.d_out - n0 : BN;
     const int64_t w0 = static_cast<int64_t>(r.group) * a.d_out + n0;
@@ -269,29 +269,25 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
             send[g] = (x ? a.ex : a.ew) + ((bytes - 1) & ~int64_t{3});
         }
     }
-    const uint32_t ring = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds_addr(&lds[wave][0])));
-    auto issue = [&](int chunk, int st) {
-        const uint32_t at = ring + static_cast<uint32_t>(st * kStageBytes);
-        uint32_t col = static_cast<uint32_t>(chunk) * 64u + cu;
-        if (!ALN) col = col < rb ? col : 0;        // past the row's end: any unit of it
+    const uint32_t at0 = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(lds_addr(&lds[wave][0])));
+    uint32_t col = static_cast<uint32_t>(chunk) * 64u + cu;
+    if (!ALN) col = col < rb ? col : 0;            // past the row's end: any unit of it
 #pragma unroll
-        for (int g = 0; g < L; ++g) mx4_copy16(src[g] + col, at + g * 1024u);
+    for (int g = 0; g < L; ++g) mx4_copy16(src[g] + col, at0 + g * 1024u);
 #pragma unroll
-        for (int g = 0; g < SC; ++g) {
-            const uint8_t* p = ssrc[g] + 4 * chunk;
-            if constexpr (ALN) {
-                mx4_copy4(p, at + kScaleAt + g * 256u);
-            } else {
-                const uint64_t lo = reinterpret_cast<uint64_t>(p) & ~uint64_t{3};
-                const uint64_t end = reinterpret_cast<uint64_t>(send[g]);
-                mx4_copy4(reinterpret_cast<const uint8_t*>(lo < end ? lo : end), at + kScaleAt + g * 256u);
-                mx4_copy4(reinterpret_cast<const uint8_t*>(lo + 4 < end ? lo + 4 : end),
-                          at + kScaleAt + (SC + g) * 256u);
-            }
+    for (int g = 0; g < SC; ++g) {
+        const uint8_t* p = ssrc[g] + 4 * chunk;
+        if constexpr (ALN) {
+            mx4_copy4(p, at0 + kScaleAt + g * 256u);
+        } else {
+            const uint64_t lo = reinterpret_cast<uint64_t>(p) & ~uint64_t{3};
+            const uint64_t end = reinterpret_cast<uint64_t>(send[g]);
+            mx4_copy4(reinterpret_cast<const uint8_t*>(lo < end ? lo : end), at0 + kScaleAt + g * 256u);
+            mx4_copy4(reinterpret_cast<const uint8_t*>(lo + 4 < end ? lo + 4 : end),
+                      at0 + kScaleAt + (SC + g) * 256u);
         }
-    };
-
-    // byte of the lane's scale inside a stage, by fragment
+    }
+    // byte of the lane's scale, by fragment
     int sat[L];
 #pragma unroll
     for (int g = 0; g < L; ++g) {
@@ -306,59 +302,31 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
         }
         sat[g] = kScaleAt + dword * (SC * 256) + 4 * i + byte;
     }
+    wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
     const int slot = 16 * (4 * l16 + (q ^ (l16 >> 2)));
     u32x4 f[L];
     int s[L];
-    auto read = [&](int st) {
-        const uint8_t* at = &lds[wave][st * kStageBytes];
+#pragma unroll
+    for (int g = 0; g < L; ++g) {
+        f[g] = *reinterpret_cast<const u32x4*>(&lds[wave][g * 1024 + slot]);
+        s[g] = lds[wave][sat[g]];
+    }
+    if (!ALN && 4 * chunk + q >= static_cast<int>(sb)) {
 #pragma unroll
         for (int g = 0; g < L; ++g) {
-            f[g] = *reinterpret_cast<const u32x4*>(at + g * 1024 + slot);
-            s[g] = at[sat[g]];
+            s[g] = kMxByteOne;
+            f[g] = u32x4{0u, 0u, 0u, 0u};
         }
-    };
+    }
     f32x4 acc[A][B];
 #pragma unroll
     for (int i = 0; i < A; ++i)
 #pragma unroll
-        for (int j = 0; j < B; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    auto compute = [&](int chunk) {
-        if (!ALN && 4 * chunk + q >= static_cast<int>(sb)) {
-#pragma unroll
-            for (int g = 0; g < L; ++g) {
-                s[g] = kMxByteOne;
-                f[g] = u32x4{0u, 0u, 0u, 0u};
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < A; ++i)
-#pragma unroll
-            for (int j = 0; j < B; ++j) acc[i][j] = mx4_mfma(f[A + j], f[i], acc[i][j], s[A + j], s[i]);
-    };
-    const int cnt = nk > wave ? (nk - wave + kSpWaves - 1) / kSpWaves : 0;
-#pragma unroll
-    for (int st = 0; st < D; ++st)
-        if (st < cnt) issue(wave + st * kSpWaves, st);
-    int i = 0, st = 0;
-    for (; i + D < cnt; ++i) {
-        wait_vmcnt<(D - 1) * COPIES>();
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("" ::: "memory");
-        read(st);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        issue(wave + (i + D) * kSpWaves, st);
-        compute(wave + i * kSpWaves);
-        st = st + 1 == D ? 0 : st + 1;
-    }
-    wait_vmcnt<0>();
-    asm volatile("" ::: "memory");
-    for (; i < cnt; ++i) {
-        read(st);
-        compute(wave + i * kSpWaves);
-        st = st + 1 == D ? 0 : st + 1;
-    }
+        for (int j = 0; j < B; ++j)
+            acc[i][j] = mx4_mfma(f[A + j], f[i], f32x4{0.0f, 0.0f, 0.0f, 0.0f}, s[A + j], s[i]);
 
-    mx4_join<Y, A, B, kSpWaves>(a, r, n0, lds, acc);
+    mx4_join<Y, A, B, kSpWaves>(a, r, n0, static_cast<int>(blockDim.x) / kWave, lds, acc);
 }
 
 // The same with whole cache lines, for rows of at least 512 elements: a chunk
@@ -383,7 +351,7 @@ constexpr int ln_wave_bytes(int a, int b, int d, int w) {      // as many scale 
 
 template <typename Y, int A, int B, int D, int W, bool EX>
 __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r, int n0,
-                                              uint8_t (&lds)[W][ln_wave_bytes(A, B, D, W)]) {
+                                              uint8_t (*lds)[ln_wave_bytes(A, B, D, W)]) {
     constexpr int BM = 16 * A, BN = 16 * B;
     constexpr int L = A + B;
     constexpr int SC = (L + 1) / 2;        // scale copies per window
@@ -595,7 +563,7 @@ __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r
         st = st + 1 == D ? 0 : st + 1;
     }
 
-    mx4_join<Y, A, B, W>(a, r, n0, lds, acc);
+    mx4_join<Y, A, B, W>(a, r, n0, W, lds, acc);
 }
 
 // Tiles of the call, walked so that XCD x (workgroups are dealt to the 8 of
@@ -621,10 +589,11 @@ __device__ __forceinline__ void mx4_walk(const Mx4Args& a, F tile) {
     }
 }
 
-template <typename Y, int A, int B, int D, bool ALN>
-__global__ __launch_bounds__(kSpThreads) void mx4_split_kernel(Mx4Args a) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kSpWaves][sp_wave_bytes(A, B, D, ALN)];
-    mx4_walk<16 * A, 16 * B>(a, [&](const Mx4Rows& r, int n0) { mx4_split_tile<Y, A, B, D, ALN>(a, r, n0, lds); });
+template <typename Y, int A, int B, bool ALN>
+__global__ __launch_bounds__(kSpWaves * kWave) void mx4_split_kernel(Mx4Args a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t dynamic_lds[];
+    uint8_t (*const lds)[sp_wave_bytes(A, B, ALN)] = reinterpret_cast<uint8_t (*)[sp_wave_bytes(A, B, ALN)]>(dynamic_lds);
+    mx4_walk<16 * A, 16 * B>(a, [&](const Mx4Rows& r, int n0) { mx4_split_tile<Y, A, B, ALN>(a, r, n0, lds); });
 }
 
 template <typename Y, int A, int B, int D, int W, bool EX>
@@ -1100,8 +1069,8 @@ __global__ __launch_bounds__(kTlThreads, BN == 128 ? 2 : 1) void mx4_tile_kernel
 }
 
 // ---------------------------------------------------------------- dispatch
-// Tile shapes of the split kernel: rows / 16, outputs / 16, ring chunks.
-#define CAT_SPLIT_TILES(V) V(0, 1, 1, 4) V(1, 1, 2, 4) V(2, 1, 4, 3) V(3, 2, 4, 2) V(4, 4, 4, 2)
+// Tile shapes of the split kernel: rows / 16, outputs / 16.
+#define CAT_SPLIT_TILES(V) V(0, 1, 1) V(1, 1, 2) V(2, 1, 4) V(3, 2, 4) V(4, 4, 4)
 // Of the line kernel: rows / 16, outputs / 16, ring chunks, waves.
 #define CAT_LINE_TILES(V) \
     V(0, 1, 1, 2, 8) V(1, 1, 2, 2, 4) V(2, 1, 4, 1, 4) V(3, 2, 2, 2, 4) V(4, 2, 4, 1, 4) V(5, 3, 4, 1, 4) \
@@ -1109,7 +1078,7 @@ __global__ __launch_bounds__(kTlThreads, BN == 128 ? 2 : 1) void mx4_tile_kernel
 struct SmallTile {
     int a, b, d, w;
 };
-#define CAT_SHAPE(id, A, B, D) {A, B, D, kSpWaves},
+#define CAT_SHAPE(id, A, B) {A, B, 1, kSpWaves},
 static constexpr SmallTile kSpTiles[] = {CAT_SPLIT_TILES(CAT_SHAPE)};
 #undef CAT_SHAPE
 #define CAT_SHAPE(id, A, B, D, W) {A, B, D, W},
@@ -1126,11 +1095,12 @@ static unsigned small_grid(const Mx4Args& a, int bm, int bn) {
 
 template <typename Y, bool ALN>
 static hipError_t launch_split(const Mx4Args& a, int tile, hipStream_t stream) {
+    const int waves = (a.d_in + 127) / 128;
     switch (tile) {
-#define CAT_CASE(id, A, B, D)                                                             \
+#define CAT_CASE(id, A, B)                                                                \
     case id:                                                                              \
-        mx4_split_kernel<Y, A, B, D, ALN>                                                 \
-            <<<small_grid(a, 16 * A, 16 * B), kSpThreads, 0, stream>>>(a);                \
+        mx4_split_kernel<Y, A, B, ALN><<<small_grid(a, 16 * A, 16 * B), waves * kWave,    \
+                                         waves * sp_wave_bytes(A, B, ALN), stream>>>(a);  \
         break;
         CAT_SPLIT_TILES(CAT_CASE)
 #undef CAT_CASE
@@ -1202,13 +1172,15 @@ static double tile_cost(const Mx4Args& a, int bm, int bn, int cus) {
     const double rounds = std::ceil(tiles / cus);
     return bm == 128 ? rounds * (970.0 * pairs + 5940.0) + 120.0 : rounds * (1360.0 * pairs + 8630.0) - 500.0;
 }
-// Short rows (the split kernel): all its waves together hold the whole
-// reduction, so a tile is a fixed part, its copies and its sums.  2.7% over
-// the fastest of the five at 200 random shapes.
+// Short rows (the split kernel): one chunk's latency, and per tile of a CU its
+// copies and sums.  0.6% over the fastest of the five at 400 random shapes (1
+// to 16384 rows, dense and by up to 64 experts, 32 to 480 inputs, 32 to 16384
+// outputs).
 static double split_cost(const Mx4Args& a, const SmallTile& t, int cus) {
     const int l = t.a + t.b, copies = l + (l + 3) / 4 * (a.d_in % 128 == 0 ? 1 : 2);
     const double tiles = row_tiles(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
-    return std::ceil(tiles / cus) * (10.0 * ((a.d_in + 127) / 128) * copies + 50.0 * t.a * t.b + 1200.0);
+    const double work = 16.7 * ((a.d_in + 127) / 128) * copies + 25.5 * t.a * t.b;
+    return 3200.0 + 29.0 * copies + 85.0 * t.a * t.b + tiles / cus * work;
 }
 
 // CUs of the current device, asked once a device: the question takes 0.3 us of
@@ -1239,7 +1211,7 @@ static hipError_t launch(const Mx4Args& a, hipStream_t stream) {
             pick = id;
         }
     };
-    if (a.d_in < 512) {
+    if (a.d_in < kSpRow) {
         constexpr int n = sizeof(kSpTiles) / sizeof(kSpTiles[0]);
         for (int i = 0; i < n; ++i) offer(i, split_cost(a, kSpTiles[i], cus));
         return a.d_in % 128 == 0 ? launch_split<Y, true>(a, pick, stream) : launch_split<Y, false>(a, pick, stream);
