@@ -8,7 +8,7 @@
 // The order of the reduction is free as long as both operands take the same,
 // which every kernel here uses to load whole pieces of rows.
 //
-// Three forms, picked by an estimate of their times (at the end):
+// Three forms, picked by an estimate of their times (mx4_pick.h):
 //   line   few rows: small tiles, their reduction shared out among the waves of
 //          a workgroup; bound by the weights' bytes
 //   tile   many rows: 128 x 128, 128 x 256 or 256 x 256 outputs a workgroup;
@@ -23,11 +23,11 @@
 //   -> 1024 9.5 us, 16384 rows of 8 uneven experts 14336 -> 4096 506 to 530 us
 //   (3.6 to 3.8).
 #include <atomic>
-#include <cmath>
 #include <type_traits>
 
 #include "kernels.h"
 #include "mx4_common.h"
+#include "mx4_pick.h"
 
 namespace catk {
 
@@ -177,19 +177,6 @@ __device__ __forceinline__ void mx4_copy4(const uint8_t* p, uint32_t lds) {
 //
 // 8192 x 256 -> 4096 27 us and 1000 x 480 -> 4096 8.5; with eight waves of
 // which half or more had no chunk, and a ring for each, 92 and 16.
-constexpr int kSpWaves = 4;                // at most
-constexpr int kSpRow = 512;                // elements that a row has less of
-static_assert(kSpRow == 128 * kSpWaves, "a wave for each chunk, none without");
-
-// Accumulators whose partial sums are added at a time: one per wave.
-constexpr int mx4_round(int a, int b, int w) { return a * b < w ? a * b : w; }
-// LDS of a wave: its copies, later its partial sums of a round.
-constexpr int mx4_wave_bytes(int a, int b, int w, int ring) {
-    return ring > mx4_round(a, b, w) * 1024 ? ring : mx4_round(a, b, w) * 1024;
-}
-constexpr int sp_wave_bytes(int a, int b, bool aligned) {
-    return mx4_wave_bytes(a, b, kSpWaves, (a + b) * 1024 + (a + b + 3) / 4 * 256 * (aligned ? 1 : 2));
-}
 
 // Adds the partial sums of the workgroup's waves (W at most) in the waves'
 // order through LDS and stores them.
@@ -343,12 +330,6 @@ __device__ __forceinline__ void mx4_split_tile(const Mx4Args& a, const Mx4Rows& 
 // dword that holds the first one's first byte; each half of them is moved back
 // where it would pass the buffer's last dword, and a lane finds its bytes in
 // it; units past a row's end count as zero with scale 1.
-constexpr int ln_scale_bytes(int a, int b) { return (a + b + 1) / 2 * 1024; }
-constexpr int ln_stage_bytes(int a, int b) { return 2 * (a + b) * 1024; }
-constexpr int ln_wave_bytes(int a, int b, int d, int w) {      // as many scale buffers as chunks
-    return mx4_wave_bytes(a, b, w, d * (ln_stage_bytes(a, b) + ln_scale_bytes(a, b)));
-}
-
 template <typename Y, int A, int B, int D, int W, bool EX>
 __device__ __forceinline__ void mx4_line_tile(const Mx4Args& a, const Mx4Rows& r, int n0,
                                               uint8_t (*lds)[ln_wave_bytes(A, B, D, W)]) {
@@ -1069,22 +1050,6 @@ __global__ __launch_bounds__(kTlThreads, BN == 128 ? 2 : 1) void mx4_tile_kernel
 }
 
 // ---------------------------------------------------------------- dispatch
-// Tile shapes of the split kernel: rows / 16, outputs / 16.
-#define CAT_SPLIT_TILES(V) V(0, 1, 1) V(1, 1, 2) V(2, 1, 4) V(3, 2, 4) V(4, 4, 4)
-// Of the line kernel: rows / 16, outputs / 16, ring chunks, waves.
-#define CAT_LINE_TILES(V) \
-    V(0, 1, 1, 2, 8) V(1, 1, 2, 2, 4) V(2, 1, 4, 1, 4) V(3, 2, 2, 2, 4) V(4, 2, 4, 1, 4) V(5, 3, 4, 1, 4) \
-    V(6, 4, 4, 1, 4)
-struct SmallTile {
-    int a, b, d, w;
-};
-#define CAT_SHAPE(id, A, B) {A, B, 1, kSpWaves},
-static constexpr SmallTile kSpTiles[] = {CAT_SPLIT_TILES(CAT_SHAPE)};
-#undef CAT_SHAPE
-#define CAT_SHAPE(id, A, B, D, W) {A, B, D, W},
-static constexpr SmallTile kLnTiles[] = {CAT_LINE_TILES(CAT_SHAPE)};
-#undef CAT_SHAPE
-
 // A launch covers fewer than 2^32 threads; workgroups then take several tiles.
 constexpr int64_t kSpMaxGrid = int64_t{1} << 22;
 static unsigned small_grid(const Mx4Args& a, int bm, int bn) {
@@ -1131,58 +1096,6 @@ static hipError_t launch_tiles(const Mx4Args& a, int cus, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Row tiles to expect.  Where rows go is known on the device only: their
-// counts are taken as exponentially distributed over the experts that have
-// any (a router prefers some), which gives 1 / (1 - exp(-bm / mean)) tiles each.
-static double row_tiles(const Mx4Args& a, int bm) {
-    if (!a.offsets) return static_cast<double>((a.m + bm - 1) / bm);
-    const double used = a.groups * (1.0 - std::exp(-static_cast<double>(a.m) / a.groups));
-    return used / (1.0 - std::exp(-bm * used / a.m));
-}
-
-// Estimated nanoseconds.  Small tiles: the workgroups of a CU that fit its LDS
-// and waves run together, so a CU's tiles cost their rounds at the latency of
-// the chunks of a wave (580 ns each, 360 with two in flight) or their sum at
-// the rate of its copies (13.9 ns each) and of the sums, whichever is longer.
-// Large tiles: rounds, pairs and a fixed part; 128 x 128 outputs run two a CU,
-// a pair of both in 1.2 us where one alone takes 0.64.  Over 700 random shapes
-// (1 to 4096 rows, dense and by up to 128 experts, 1024 to 14336 inputs, 128 to
-// 16384 outputs) the shape with the least estimate took 2.5% longer than the
-// fastest of the ten.
-static double line_cost(const Mx4Args& a, const SmallTile& t, int cus) {
-    const int l = t.a + t.b, pieces = (a.d_in + 255) / 256;
-    const double copies = 2 * l + 0.25 * ((l + 1) / 2);
-    const int wave_bytes = ln_wave_bytes(t.a, t.b, t.d, t.w);
-    const int by_lds = 160 * 1024 / (wave_bytes * t.w), by_waves = (l > 5 ? 16 : 24) / t.w;
-    const int together = by_lds < by_waves ? by_lds : by_waves;
-    const double tiles = row_tiles(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
-    const double per_cu = std::ceil(tiles / cus), rounds = std::ceil(per_cu / together);
-    const double latency = 1360.0 + (t.d == 2 ? 360.0 : 580.0) * ((pieces + t.w - 1) / t.w) + 6.0 * copies;
-    const double work = 13.9 * pieces * copies + 71.0 * t.a * t.b + 570.0;
-    const double by_work = per_cu * work + 900.0;
-    return 1560.0 + (rounds * latency > by_work ? rounds * latency : by_work);
-}
-static double tile_cost(const Mx4Args& a, int bm, int bn, int cus) {
-    const int pairs = (a.d_in + 511) / 512 * 2;
-    const double tiles = row_tiles(a, bm) * ((a.d_out + bn - 1) / bn);
-    if (bn == 128) {
-        const double full = std::ceil(tiles / (2 * cus)) - 1.0, rest = tiles - full * 2 * cus;
-        return full * (1198.0 * pairs + 4270.0) + (rest > cus ? 1198.0 * pairs + 4270.0 : 640.0 * pairs + 4310.0);
-    }
-    const double rounds = std::ceil(tiles / cus);
-    return bm == 128 ? rounds * (970.0 * pairs + 5940.0) + 120.0 : rounds * (1360.0 * pairs + 8630.0) - 500.0;
-}
-// Short rows (the split kernel): one chunk's latency, and per tile of a CU its
-// copies and sums.  0.6% over the fastest of the five at 400 random shapes (1
-// to 16384 rows, dense and by up to 64 experts, 32 to 480 inputs, 32 to 16384
-// outputs).
-static double split_cost(const Mx4Args& a, const SmallTile& t, int cus) {
-    const int l = t.a + t.b, copies = l + (l + 3) / 4 * (a.d_in % 128 == 0 ? 1 : 2);
-    const double tiles = row_tiles(a, 16 * t.a) * ((a.d_out + 16 * t.b - 1) / (16 * t.b));
-    const double work = 16.7 * ((a.d_in + 127) / 128) * copies + 25.5 * t.a * t.b;
-    return 3200.0 + 29.0 * copies + 85.0 * t.a * t.b + tiles / cus * work;
-}
-
 // CUs of the current device, asked once a device: the question takes 0.3 us of
 // a call's 4.
 static hipError_t device_cus(int& cus) {
@@ -1198,37 +1111,28 @@ static hipError_t device_cus(int& cus) {
     return err;
 }
 
+template <typename Y, bool EX>
+static hipError_t launch_tile(const Mx4Args& a, int shape, int cus, hipStream_t stream) {
+    if (shape == 0) return launch_tiles<Y, 128, 128, EX>(a, cus, stream);
+    if (shape == 1) return launch_tiles<Y, 128, 256, EX>(a, cus, stream);
+    return launch_tiles<Y, 256, 256, EX>(a, cus, stream);
+}
+
 template <typename Y>
 static hipError_t launch(const Mx4Args& a, hipStream_t stream) {
     int cus = 0;
     const hipError_t err = device_cus(cus);
     if (err != hipSuccess) return err;
-    int pick = 0;
-    double best = 0.0;
-    auto offer = [&](int id, double cost) {
-        if (id == 0 || cost < best) {
-            best = cost;
-            pick = id;
-        }
-    };
-    if (a.d_in < kSpRow) {
-        constexpr int n = sizeof(kSpTiles) / sizeof(kSpTiles[0]);
-        for (int i = 0; i < n; ++i) offer(i, split_cost(a, kSpTiles[i], cus));
-        return a.d_in % 128 == 0 ? launch_split<Y, true>(a, pick, stream) : launch_split<Y, false>(a, pick, stream);
+    const Mx4Sizes z{a.n, a.m, a.groups, a.d_in, a.d_out, a.offsets != nullptr, a.row_ids != nullptr};
+    const Mx4Pick p = mx4_pick(z, cus);
+    switch (p.form) {
+        case Mx4Form::split:
+            return p.whole ? launch_split<Y, true>(a, p.shape, stream) : launch_split<Y, false>(a, p.shape, stream);
+        case Mx4Form::line:
+            return p.whole ? launch_line<Y, true>(a, p.shape, stream) : launch_line<Y, false>(a, p.shape, stream);
+        case Mx4Form::tile: break;
     }
-    constexpr int n = sizeof(kLnTiles) / sizeof(kLnTiles[0]);
-    for (int i = 0; i < n; ++i) offer(i, line_cost(a, kLnTiles[i], cus));
-    // the large tiles take 32-bit offsets into gathered rows
-    if (!a.row_ids || static_cast<int64_t>(a.n) * (a.d_in / 2) < (int64_t{1} << 32)) {
-        offer(n, tile_cost(a, 128, 128, cus));
-        offer(n + 1, tile_cost(a, 128, 256, cus));
-        offer(n + 2, tile_cost(a, 256, 256, cus));
-    }
-    const bool ex = a.d_in % 512 == 0;     // of the large tiles; rows of whole chunks for the line kernel
-    if (pick == n) return ex ? launch_tiles<Y, 128, 128, true>(a, cus, stream) : launch_tiles<Y, 128, 128, false>(a, cus, stream);
-    if (pick == n + 1) return ex ? launch_tiles<Y, 128, 256, true>(a, cus, stream) : launch_tiles<Y, 128, 256, false>(a, cus, stream);
-    if (pick == n + 2) return ex ? launch_tiles<Y, 256, 256, true>(a, cus, stream) : launch_tiles<Y, 256, 256, false>(a, cus, stream);
-    return a.d_in % 256 == 0 ? launch_line<Y, true>(a, pick, stream) : launch_line<Y, false>(a, pick, stream);
+    return p.whole ? launch_tile<Y, true>(a, p.shape, cus, stream) : launch_tile<Y, false>(a, p.shape, cus, stream);
 }
 
 hipError_t launch_mx4_linear(const uint8_t* cx, const uint8_t* ex, const uint8_t* cw,
