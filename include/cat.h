@@ -493,8 +493,9 @@ int cat_mx4_dequant(const uint8_t* codes, const uint8_t* scales, int64_t n,
  *   y[t, o] = sum_j x[t, j] * w[o, j]
  * of the values the codes stand for; products are exact, sums fp32 (in an
  * order that depends on the sizes only: repeated calls give identical
- * bits), y rounded once to y_dtype.  Sums beyond fp32's range are infinite,
- * or NaN where infinities of both signs meet; below it they round to 0.
+ * bits), y rounded once to y_dtype.  y is infinite or NaN where the sum goes
+ * beyond fp32's range, and may be where a part of it does (the order decides);
+ * subnormal sums are kept, smaller ones round to 0.
  * codes_x  device uint8 [n x d_in/2], scales_x device uint8 [n x d_in/32].
  * codes_w  device uint8 [d_out x d_in/2], scales_w device uint8
  *          [d_out x d_in/32].
