@@ -428,11 +428,12 @@ int cat_sqnr_terms(const float* s_x, int64_t n, int bits_x,
  *   code = clamp(rint(fl(y * fl(127 / amax))), -127, 127)): the operand of
  *   cat_int8_linear.  A token with amax < 127 * 2^-128 (about 3.7e-37: 0, or
  *   so small that 127 / amax overflows) gets s_x = 0 and zero codes;
- *   one with a NaN or an infinity in h (or in fl(h * weight)) gets s_x = NaN
+ *   one with a NaN or an infinity in h, fl(h * weight) or y gets s_x = NaN
  *   and zero codes, so that its outputs are NaN.
  * cat_rmsnorm_mx4: MXFP4 codes and scales of y with the arithmetic of
  *   cat_mx4_quant: the operand of cat_mx4_linear.  A token with a NaN or an
- *   infinity in h gets the scale byte 255 (NaN) and zero codes throughout.
+ *   infinity in h gets the scale byte 255 (NaN) and zero codes throughout; one
+ *   in fl(h * weight) or y alone, in its block.
  *
  * x         device [n x d], x_dtype.  n >= 1; d >= 1, and d % 32 == 0 for
  *           cat_rmsnorm_mx4.
@@ -503,8 +504,10 @@ int cat_mx4_dequant(const uint8_t* codes, const uint8_t* scales, int64_t n,
  *          CAT_MAX_D_IN.
  * y        device y_dtype [n x d_out] (written; no overlap with inputs).
  * A scale byte of 255 makes every output of its row (or column) NaN.
- * Pointers are 16-byte aligned.  No workspace.  The call may be captured
- * into a HIP graph.
+ * Pointers are 16-byte aligned.  Where d_in % 128 != 0 scales are read in
+ * aligned 4-byte words: of a scales buffer whose size is no multiple of 4 the
+ * up to 3 bytes behind it in its last word are read too, and not used.
+ * No workspace.  The call may be captured into a HIP graph.
  * Errors: CAT_ERR_INVALID_ARG, CAT_ERR_UNSUPPORTED (d_in, n or d_out beyond
  * the limits), CAT_ERR_HIP.
  */
@@ -530,7 +533,8 @@ int cat_mx4_linear(const uint8_t* codes_x, const uint8_t* scales_x,
  * offsets and row_ids are read on the device, so the call needs no
  * synchronisation and may be captured and replayed with other values; n, m
  * and the values are not checked against each other there.  Values outside
- * the ranges above give undefined rows, but no access outside the buffers.
+ * the ranges above give undefined rows, but no access outside the buffers
+ * (other than the read at a scales buffer's end, as in cat_mx4_linear).
  * m <= 2^30.  Other arguments and errors as cat_mx4_linear.
  */
 #define CAT_MAX_GROUPS 4096

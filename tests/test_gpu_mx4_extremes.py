@@ -102,3 +102,21 @@ def test_nan_scale_beside_every_scale(n, d_in, d_out):
         sx[1, d_in // 32 - 1] = 255
         got = np.isnan(_product(cx, sx, cw, sw, "f32"))
         assert got[1].all() and (bw == 254 or not (got[0].any() or got[2:].any()))
+
+
+@pytest.mark.parametrize("d_in", [32, 96, 160, 288, 352, 480, 544, 672])
+@pytest.mark.parametrize("n,d_out", [(1, 1), (3, 5), (37, 43), (601, 507)])
+def test_bytes_behind_a_scale_buffer_reach_no_result(n, d_out, d_in):
+    # the scales' last word may be read past the buffer's end: NaN bytes there
+    torch = torch_mod()
+    cx, sx = _codes(n, d_in, 1, 118, 136)
+    cw, sw = _codes(d_out, d_in, 2, 118, 136)
+    views = []
+    for a in (sx, sw):
+        pad = torch.full((a.size + 64,), 255, dtype=torch.uint8, device="cuda")
+        pad[:a.size] = _dev(a.reshape(-1))
+        views.append(pad[:a.size].view(a.shape))
+    y = torch.full((n, d_out), 7.0, device="cuda")
+    _cat().cat_mx4_linear(_dev(cx), views[0], _dev(cw), views[1], y)
+    ref, absum = mo.linear(cx, sx, cw, sw)
+    assert (np.abs(y.double().cpu().numpy() - ref) <= (d_in / 32 + 16) * 2.0 ** -23 * absum).all()
