@@ -4,7 +4,8 @@
 //
 // Both kernels read every input byte and write every output byte once, so
 // they are bound by HBM at large sizes (235 M fp32 values 214 us, 5.0 TB/s;
-// back to bf16 101 us, 5.9; a copy reaches 5.1) and by the launch at small ones
+// back to bf16 101 to 113 us, 5.9 to 5.3, the codes partly or not in the
+// last-level cache, back to fp32 199 us, 5.3; a copy reaches 5.1) and by the launch at small ones
 // (257 x 14336 bf16 3.2 and 3.6 us, from the last-level cache).  A thread owns
 // eight consecutive elements (16 or 32 bytes in, 4 bytes of codes out), four
 // consecutive lanes a block, whose largest magnitude they find with two quad

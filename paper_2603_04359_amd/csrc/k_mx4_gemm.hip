@@ -12,16 +12,17 @@
 //   line   few rows: small tiles, their reduction shared out among the waves of
 //          a workgroup; bound by the weights' bytes
 //   tile   many rows: 128 x 128, 128 x 256 or 256 x 256 outputs a workgroup;
-//          bound by the copies and the matrix rate, which the power of random data holds at 6.6 to 7
-//          PFLOP/s of the nominal 10
+//          bound by the copies and the matrix rate, which the power of random
+//          data holds at 6.9 to 7.05 PFLOP/s of the nominal 10 (a loop of the
+//          instruction alone; 6.0 is the prompt's loop without its copies)
 //   split  rows of less than 512 elements, a wave for each 128 of them; bound
 //          by the outputs' bytes
 // Kernel times, weights in the last-level cache (rows x inputs -> outputs):
-//   1 x 4096 -> 4096 3.4 us, 48 x 4096 -> 14336 7.1 us, 100 x 4096 -> 4096
-//   5.8 us, 257 x 14336 -> 4096 22 us, 1000 x 4096 -> 4096 17 us, 8192 x 4096
-//   -> 14336 220 to 250 us (3.8 to 4.4 PFLOP/s); 128 rows of 64 experts 2048
-//   -> 1024 9.5 us, 16384 rows of 8 uneven experts 14336 -> 4096 506 to 530 us
-//   (3.6 to 3.8).
+//   1 x 4096 -> 4096 3.5 us, 48 x 4096 -> 14336 7.1 to 7.5, 100 x 4096 -> 4096
+//   5.9, 257 x 14336 -> 4096 22, 1000 x 4096 -> 4096 15 to 16.5, 8192 x 4096
+//   -> 14336 220 to 250 (3.8 to 4.4 PFLOP/s), 8192 x 256 -> 4096 27; 128 rows of
+//   64 experts 2048 -> 1024 9.5, 16384 rows of 8 uneven experts 14336 -> 4096
+//   506 to 530 (3.6 to 3.8).
 #include <atomic>
 #include <type_traits>
 

@@ -76,10 +76,11 @@ inline double row_tiles(const Mx4Sizes& a, int bm) {
 // the chunks of a wave (580 ns each, 360 with two in flight) or their sum at
 // the rate of its copies (13.9 ns each) and of the sums, whichever is longer.
 // Large tiles: rounds, pairs and a fixed part; 128 x 128 outputs run two a CU,
-// a pair of both in 1.2 us where one alone takes 0.64.  Over 700 random shapes
+// a pair of both in 1.2 us where one alone takes 0.64.  Over 800 random shapes
 // (1 to 4096 rows, dense and by up to 128 experts, 1024 to 14336 inputs, 128 to
-// 16384 outputs) the shape with the least estimate took 2.5% longer than the
-// fastest of the ten.
+// 16384 outputs) the shape with the least estimate took 2.7% longer than the
+// fastest of the ten.  The estimate orders them; its own value is further off
+// (257 x 14336 -> 4096 28.7 us, measured 22).
 inline double line_cost(const Mx4Sizes& a, const SmallTile& t, int cus) {
     const int l = t.a + t.b, pieces = (a.d_in + 255) / 256;
     const double copies = 2 * l + 0.25 * ((l + 1) / 2);
