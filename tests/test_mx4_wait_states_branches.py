@@ -93,7 +93,8 @@ MFMA = "v_mfma_scale_f32_16x16x128_f8f6f4 a[0:3], v[0:3], v[4:7], a[0:3], v8, v9
 @pytest.mark.parametrize("body,count", [
     # a result at the end of a loop, read by its first matrix instruction
     ("v_mov_b32 v0, 0\ns_nop 1\n.L1:\n" + MFMA + "\ns_nop 15\nv_add_u32 v8, v8, v1\ns_cbranch_scc1 .L1\ns_endpgm", 1),
-    ("v_mov_b32 v0, 0\ns_nop 1\n.L1:\n" + MFMA + "\ns_nop 15\nv_add_u32 v8, v8, v1\ns_nop 0\ns_cbranch_scc1 .L1\ns_endpgm", 0),
+    ("v_mov_b32 v0, 0\ns_nop 1\n.L1:\n" + MFMA + "\ns_nop 15\nv_add_u32 v8, v8, v1\ns_nop 0\n"
+     "s_cbranch_scc1 .L1\ns_endpgm", 0),
     # what stands above a label behind an unconditional branch does not run before it
     ("s_cbranch_scc0 .L2\ns_nop 1\nv_mov_b32 v0, 0\ns_branch .L3\n.L2:\n" + MFMA + "\n.L3:\ns_endpgm", 0),
     # a sum read too early on one of two paths, and again by a matrix instruction
